@@ -325,6 +325,136 @@ enum {
 };
 RD_API int redrafter_route_counts(const rd_handle* h, int64_t* out, int32_t n);
 
+/* ------------------------------------------------------------------------------------------------------------------------
+ * A key-value cache in pages, and what reads it (the paper has no counterpart: it names no cache at all; Section 3.4's
+ * accept step compacts this cache as it does the contiguous one).
+ *
+ * A cache holds, for every layer, K and V of fixed pages of page_size tokens; a page holds all heads of those tokens, and a
+ * sequence is a row of the page table that names its pages in order.  Sequences may share pages (a common prompt, the
+ * candidates of a beam).  All state lies in device buffers of the caller's and is read and changed on the device alone:
+ *   pool       [n_layers][2 (K, V)][n_pages][n_kv_heads][page_size][head_dim] of dtype, 256-byte aligned;
+ *   page_table [max_seqs][max_seq_pages]  pages of a sequence; -1 behind its last page and where one has been trimmed;
+ *   lens       [max_seqs]  tokens of a sequence; it holds the pages ceil(lens / page_size);
+ *   refs       [n_pages]   how many entries of the table name the page;
+ *   free_bits  [(n_pages + 31) / 32]  bit p of word p / 32 set: page p is free (refs == 0).
+ * Pages are given out lowest index first, in the order of a call's sequences: what a call leaves does not depend on timing.
+ *
+ * The calls on one handle are issued in stream order on one stream at a time (their scratch is the handle's workspace; that
+ * goes for graphs that captured them, too).  All of them may be captured.  A list of sequences `seqs` is a device array of
+ * n rows of the table, or NULL: 0 .. n-1.  What a kernel finds out of range -- a sequence outside the table, a length, a
+ * page, a row, a sequence named twice by a call that changes it -- it leaves out, and the next redrafter_pages_poll
+ * reports it.  Errors of every call: INVALID_ARG, SHAPE, CUDA, STATE (another device than the handle's is current). */
+typedef struct {
+  int32_t struct_bytes;                       /* sizeof(rd_page_cache) */
+  int32_t n_layers, n_kv_heads, head_dim;     /* head_dim 64 or 128 */
+  int32_t dtype;                              /* RD_DTYPE_* of the pool, and of the rows written to it and read against it */
+  int32_t page_size;                          /* tokens: 16, 32, 64 or 128 */
+  int32_t n_pages, max_seqs, max_seq_pages;   /* n_layers * 2 * n_pages * n_kv_heads * page_size < 2^31 */
+  int32_t reserved;
+  void* pool;
+  int32_t* page_table;
+  int32_t* lens;
+  int32_t* refs;
+  uint32_t* free_bits;
+} rd_page_cache;
+
+typedef struct rd_pages rd_pages;
+
+/* Bytes of the pool and of the device workspace of a handle on it (0 if a size is out of range); the buffers of `cache` are not looked at. */
+RD_API size_t redrafter_pages_pool_bytes(const rd_page_cache* cache);
+RD_API size_t redrafter_pages_workspace_bytes(const rd_page_cache* cache);
+
+/* Create a handle on the cache's buffers, whose contents stay as they are (redrafter_pages_reset empties a new cache).
+ * `workspace` is a 256-byte aligned device pointer that the handle uses until it is destroyed.  Waits for the work it
+ * enqueues on stream 0.  Errors: INVALID_ARG, SHAPE, CAPACITY (workspace too small), CUDA. */
+RD_API int redrafter_pages_init(const rd_page_cache* cache, void* workspace, size_t ws_bytes, rd_pages** out);
+RD_API int redrafter_pages_destroy(rd_pages* h);
+
+/* Message of the last failing call on this handle; with h == NULL: why the last redrafter_pages_init failed. */
+RD_API const char* redrafter_pages_last_error(const rd_pages* h);
+
+/* Every page free, every sequence empty.  The pool is not touched. */
+RD_API int redrafter_pages_reset(rd_pages* h, void* stream);
+
+/* Room for n_new[i] (device [n]) more tokens of each sequence: lens grows by it, new pages are added, and a last page that
+ * is partly filled and shared is first copied for the sequence that is going to write into it (as if the sequences came one
+ * after another: the last of its sharers keeps it).  All or nothing: with too few free pages nothing changes, and the next
+ * poll returns CAPACITY. */
+RD_API int redrafter_pages_extend(rd_pages* h, const int32_t* seqs, const int32_t* n_new, int32_t n, void* stream);
+
+/* Sequence dst[i] becomes another name for the tokens of src[i]; their pages are shared, nothing is copied (device arrays
+ * [n]).  A source may be named several times; a target has to be empty, and neither named twice nor a source of the call. */
+RD_API int redrafter_pages_fork(rd_pages* h, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+/* Of the last n_rows[i] tokens of each sequence the first n_keep[i] listed ones stay (device [n] each): token
+ * rows[i * row_stride + j] of them moves to place j, in every layer, and what lies behind is given back.  The rows ascend.
+ * rows == NULL: the first n_keep ones stay, nothing moves.  This is the accept step's compaction (Section 3.4): extend by the
+ * packed rows of a verification, write and verify them, keep the accepted path.  A page that a row moves into must not be
+ * shared (extend sees to that). */
+RD_API int redrafter_pages_compact(rd_pages* h, const int32_t* seqs, const int32_t* n_rows, const int32_t* n_keep, const int32_t* rows,
+                                   int32_t row_stride, int32_t n, void* stream);
+
+/* Gives back the pages that attention with this window and these sinks no longer sees from the last token on: those wholly
+ * behind the first `sinks` tokens and wholly before token lens - window.  Lengths stay. */
+RD_API int redrafter_pages_trim(rd_pages* h, const int32_t* seqs, int32_t window, int32_t sinks, int32_t n, void* stream);
+
+/* Empties the sequences; pages that no other one names become free. */
+RD_API int redrafter_pages_free(rd_pages* h, const int32_t* seqs, int32_t n, void* stream);
+
+/* K and V of new tokens into their pages.  The rows of a call belong to n sequences: rows row_off[i] .. row_off[i + 1] - 1
+ * (device [n + 1], ascending) to entry i of the list, or, with row_off == NULL, one row to each (n_rows == n).  They are the
+ * LAST tokens of their sequences, in order: with m rows, the first of them is token lens - m (extend first).  n_rows bounds
+ * the rows; those from row_off[n] on are not looked at.  k, v: [n_rows][n_kv_heads][head_dim] of the cache's dtype, K after
+ * the rotary embedding, rows k_stride and v_stride elements apart and on 16-byte boundaries.  A sequence is named once.  Rows
+ * that would go into a shared page are left out and reported. */
+RD_API int redrafter_pages_write(rd_pages* h, int32_t layer, const int32_t* seqs, const int32_t* row_off, int32_t n, int32_t n_rows, const void* k,
+                                 int64_t k_stride, const void* v, int64_t v_stride, void* stream);
+
+/* Causal attention of the last tokens of sequences over their pages in one layer: rows as for redrafter_pages_write, so a row
+ * at position p sees the keys 0 .. p; with window > 0 only p - window + 1 .. p and the first `sinks` ones.
+ *   out_row = sum_j softmax_j(scale q_row . k_j) v_j,  query head a on key and value head a / (n_heads / n_kv_heads).
+ * q, out: [n_rows][n_heads][head_dim] of the cache's dtype, rows q_stride and out_stride elements apart and on 16-byte
+ * boundaries, not overlapping; rows behind the last sequence's are left as they are.  lse: [n_rows][n_heads] fp32, the natural
+ * logarithm of the softmax's denominator, or NULL.  scale 0: head_dim^-1/2.  max_rows: the most rows of any sequence, which
+ * picks the kernel (the rows of a sequence that brings more are left as they are and reported); 0: n_rows.  A row without keys (an empty sequence,
+ * or all its scores -inf) gives zeros and -inf.  Keys that a row does not see do not reach it, whatever they hold.  Sums and the
+ * softmax's statistics are in fp32; bf16: the weights that multiply V are rounded to bf16. */
+RD_API int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, const int32_t* row_off, int32_t n, int32_t n_rows, int32_t max_rows,
+                                     int32_t n_heads, const void* q, int64_t q_stride, void* out, int64_t out_stride, float* lse, float scale,
+                                     int32_t window, int32_t sinks, void* stream);
+
+/* Synchronise `stream`, read the handle's device status word and clear it: RD_OK, or what a kernel recorded. */
+RD_API int redrafter_pages_poll(rd_pages* h, void* stream);
+
+/* Number of kernels this handle has launched. */
+RD_API int64_t redrafter_pages_launch_count(const rd_pages* h);
+
+/* Log probabilities of given tokens, with the entropy of their distributions and the most likely tokens beside them: for row r
+ * of the call, x = logits[row_index ? row_index[r] : r] and y = x / temperature,
+ *   logprob = y[tokens[r]] - log sum_v exp(y_v),  entropy = -sum_v p_v log p_v,  p = softmax(y)
+ * and the `top` largest logits (lowest id first among equal ones) with their log probabilities.  Natural logarithms; sums in
+ * fp32; tokens of probability 0 add nothing to the entropy.  A token outside the vocabulary gives NaN; a row_index outside the
+ * logits gives NaN and ids of -1; a row with NaN, with +inf or of -inf alone has no distribution (NaN; its ids are still
+ * the largest, NaN above all).  Needs no handle and no workspace; may be captured. */
+typedef struct {
+  int32_t struct_bytes;      /* sizeof(rd_logprobs) */
+  int32_t dtype;             /* RD_DTYPE_* of the logits */
+  int32_t rows, n_logit_rows, vocab;
+  int32_t top;               /* 0 .. 64, at most vocab */
+  float temperature;         /* > 0 */
+  int32_t reserved;
+  int64_t row_stride;        /* elements between rows of the logits, >= vocab; no alignment is asked for */
+  const void* logits;        /* [n_logit_rows][vocab] */
+  const int32_t* row_index;  /* [rows] or NULL */
+  const int32_t* tokens;     /* [rows]; may be NULL without logprob */
+  float* logprob;            /* [rows] or NULL */
+  float* entropy;            /* [rows] or NULL */
+  int32_t* top_ids;          /* [rows][top] */
+  float* top_logprobs;       /* [rows][top] */
+} rd_logprobs;
+RD_API int redrafter_token_logprobs(const rd_logprobs* args, void* stream);
+RD_API const char* redrafter_token_logprobs_error(void);   /* why the last one failed */
+
 #ifdef __cplusplus
 }
 #endif

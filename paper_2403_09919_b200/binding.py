@@ -28,7 +28,12 @@ EXPORTS = ["redrafter_workspace_bytes", "redrafter_kv_bytes", "redrafter_init", 
            "redrafter_set_ctx_bound", "redrafter_poll", "redrafter_launch_count", "redrafter_profile",
            "redrafter_profile_read", "redrafter_trace", "redrafter_trace_read", "redrafter_trace_bytes",
            "redrafter_accept_static", "redrafter_selftest_wait", "redrafter_set_sampling", "redrafter_route_counts", "redrafter_last_logits", "redrafter_trace_prefetched",
-           "redrafter_last_packed_rows"]
+           "redrafter_last_packed_rows",
+           "redrafter_pages_pool_bytes", "redrafter_pages_workspace_bytes", "redrafter_pages_init", "redrafter_pages_destroy",
+           "redrafter_pages_last_error", "redrafter_pages_reset", "redrafter_pages_extend", "redrafter_pages_fork",
+           "redrafter_pages_compact", "redrafter_pages_trim", "redrafter_pages_free", "redrafter_pages_write",
+           "redrafter_pages_attention", "redrafter_pages_poll", "redrafter_pages_launch_count", "redrafter_token_logprobs",
+           "redrafter_token_logprobs_error"]
 
 ROUTES = ("att_rows16", "att_rows16_shallow", "att_rows64", "att_rows128_tc5", "att_key_split", "att_fp32", "gemm_pairs",
           "gemm_one_cta", "gemm_simt", "gemm_swiglu", "gemm_qkv", "att_keys_on_lanes")
@@ -56,6 +61,20 @@ class RdPacked(C.Structure):
 
 class RdAcceptOut(C.Structure):
     _fields_ = [("n_accept", C.c_void_p), ("best", C.c_void_p), ("tokens", C.c_void_p)]
+
+
+class RdPageCache(C.Structure):
+    _fields_ = [("struct_bytes", C.c_int32), ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_seqs", C.c_int32),
+                ("max_seq_pages", C.c_int32), ("reserved", C.c_int32), ("pool", C.c_void_p), ("page_table", C.c_void_p),
+                ("lens", C.c_void_p), ("refs", C.c_void_p), ("free_bits", C.c_void_p)]
+
+
+class RdLogprobs(C.Structure):
+    _fields_ = [("struct_bytes", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int32), ("n_logit_rows", C.c_int32),
+                ("vocab", C.c_int32), ("top", C.c_int32), ("temperature", C.c_float), ("reserved", C.c_int32),
+                ("row_stride", C.c_int64), ("logits", C.c_void_p), ("row_index", C.c_void_p), ("tokens", C.c_void_p),
+                ("logprob", C.c_void_p), ("entropy", C.c_void_p), ("top_ids", C.c_void_p), ("top_logprobs", C.c_void_p)]
 
 
 def lib():
@@ -101,6 +120,28 @@ def lib():
         L.redrafter_trace_prefetched.argtypes = [vp, vp, i32]
         L.redrafter_last_packed_rows.argtypes = [vp, vp, vp]
         L.redrafter_route_counts.argtypes = [vp, C.POINTER(C.c_int64), i32]
+        i64 = C.c_int64
+        for f in (L.redrafter_pages_pool_bytes, L.redrafter_pages_workspace_bytes):
+            f.restype = sz
+            f.argtypes = [C.POINTER(RdPageCache)]
+        L.redrafter_pages_init.argtypes = [C.POINTER(RdPageCache), vp, sz, C.POINTER(vp)]
+        L.redrafter_pages_destroy.argtypes = [vp]
+        L.redrafter_pages_last_error.restype = C.c_char_p
+        L.redrafter_pages_last_error.argtypes = [vp]
+        L.redrafter_pages_reset.argtypes = [vp, vp]
+        L.redrafter_pages_extend.argtypes = [vp, vp, vp, i32, vp]
+        L.redrafter_pages_fork.argtypes = [vp, vp, vp, i32, vp]
+        L.redrafter_pages_compact.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp]
+        L.redrafter_pages_trim.argtypes = [vp, vp, i32, i32, i32, vp]
+        L.redrafter_pages_free.argtypes = [vp, vp, i32, vp]
+        L.redrafter_pages_write.argtypes = [vp, i32, vp, vp, i32, i32, vp, i64, vp, i64, vp]
+        L.redrafter_pages_attention.argtypes = [vp, i32, vp, vp, i32, i32, i32, i32, vp, i64, vp, i64, vp, C.c_float, i32, i32, vp]
+        L.redrafter_pages_poll.argtypes = [vp, vp]
+        L.redrafter_pages_launch_count.restype = i64
+        L.redrafter_pages_launch_count.argtypes = [vp]
+        L.redrafter_token_logprobs.argtypes = [C.POINTER(RdLogprobs), vp]
+        L.redrafter_token_logprobs_error.restype = C.c_char_p
+        L.redrafter_token_logprobs_error.argtypes = []
         _lib = L
     return _lib
 
@@ -373,3 +414,195 @@ class ReDrafter:
         dt = torch.float32 if c["dtype"] == "fp32" else torch.bfloat16
         hd = c["d_model"] // c["n_heads"]
         return self.kv.view(dt).view(c["n_layers"], 2, c["max_batch"], c["n_heads"], c["max_ctx"], hd)
+
+
+def _dtype_name(t):
+    if t.dtype == torch.bfloat16:
+        return "bf16"
+    if t.dtype == torch.float32:
+        return "fp32"
+    raise ValueError(f"expected bfloat16 or float32, got {t.dtype}")
+
+
+class PagedCache:
+    """A key-value cache in pages: a handle on five device tensors, which the caller may read at any time.
+
+    pool [n_layers, 2, n_pages, n_kv_heads, page_size, head_dim] bf16 or fp32, page_table [max_seqs, max_seq_pages],
+    lens [max_seqs], refs [n_pages] and free_bits [(n_pages + 31) // 32], all int32 (free_bits: the bit pattern of uint32).
+    The constructor adopts tensors that are in use; PagedCache.empty makes new ones.
+    """
+
+    def __init__(self, pool, page_table, lens, refs, free_bits):
+        if not pool.is_cuda:
+            raise RuntimeError("PagedCache needs a CUDA device; there is no CPU path")
+        if pool.dim() != 6 or pool.shape[1] != 2 or page_table.dim() != 2:
+            raise ValueError("pool is [layers, 2, pages, kv heads, page size, head dim], page_table [sequences, pages]")
+        self.L = lib()
+        self.n_layers, _, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pool.shape
+        self.max_seqs, self.max_seq_pages = page_table.shape
+        self.device, self.dtype = pool.device, pool.dtype
+        for name, t, n in (("pool", pool, pool.numel()), ("page_table", page_table, page_table.numel()), ("lens", lens, self.max_seqs),
+                           ("refs", refs, self.n_pages), ("free_bits", free_bits, (self.n_pages + 31) // 32)):
+            if t.device != self.device or not t.is_contiguous() or t.numel() != n or (name != "pool" and t.dtype != torch.int32):
+                raise ValueError(f"{name}: expected {n} contiguous {'elements' if name == 'pool' else 'int32'} on {self.device}")
+        self.pool, self.page_table, self.lens, self.refs, self.free_bits = pool, page_table, lens, refs, free_bits
+        c = RdPageCache(C.sizeof(RdPageCache), self.n_layers, self.n_kv_heads, self.head_dim, RD_DTYPE[_dtype_name(pool)], self.page_size,
+                        self.n_pages, self.max_seqs, self.max_seq_pages, 0, pool.data_ptr(), page_table.data_ptr(), lens.data_ptr(),
+                        refs.data_ptr(), free_bits.data_ptr())
+        with torch.cuda.device(self.device):
+            ws = self.L.redrafter_pages_workspace_bytes(C.byref(c))
+            self.workspace = torch.empty(max(ws, 256), dtype=torch.uint8, device=self.device)
+            torch.cuda.current_stream().synchronize()   # the workspace is cleared on another stream
+            hp = C.c_void_p()
+            rc = self.L.redrafter_pages_init(C.byref(c), self.workspace.data_ptr(), ws, C.byref(hp))
+        if rc:
+            raise RdError(rc, "redrafter_pages_init failed: " + self.L.redrafter_pages_last_error(None).decode())
+        self.h = hp
+
+    @classmethod
+    def empty(cls, n_layers, n_kv_heads, head_dim, page_size, n_pages, max_seqs, max_seq_pages, dtype="bf16", device="cuda:0"):
+        i32 = dict(dtype=torch.int32, device=device)
+        pool = torch.empty(n_layers, 2, n_pages, n_kv_heads, page_size, head_dim, device=device,
+                           dtype=torch.float32 if dtype == "fp32" else torch.bfloat16)
+        cache = cls(pool, torch.empty(max_seqs, max_seq_pages, **i32), torch.empty(max_seqs, **i32), torch.empty(n_pages, **i32),
+                    torch.empty((n_pages + 31) // 32, **i32))
+        cache.reset()
+        return cache
+
+    def close(self):
+        if getattr(self, "h", None):
+            self.L.redrafter_pages_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _ck(self, rc):
+        if rc:
+            raise RdError(rc, self.L.redrafter_pages_last_error(self.h).decode())
+
+    def _stream(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _list(self, name, t, n=None):
+        """Pointer of a device list of whole numbers (None stays None)."""
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous() or (n is not None and t.numel() != n):
+            raise ValueError(f"{name}: expected {'a list of' if n is None else n} contiguous int32 on {self.device}")
+        return t.data_ptr()
+
+    # ---- the C-ABI calls, same names
+    def reset(self):
+        self._ck(self.L.redrafter_pages_reset(self.h, self._stream()))
+
+    def extend(self, n_new, seqs=None):
+        """Room for n_new[i] more tokens of each sequence; a shared last page is copied for its writer."""
+        n = n_new.numel()
+        self._ck(self.L.redrafter_pages_extend(self.h, self._list("seqs", seqs, n), self._list("n_new", n_new), n, self._stream()))
+
+    def fork(self, src, dst):
+        n = src.numel()
+        self._ck(self.L.redrafter_pages_fork(self.h, self._list("src", src), self._list("dst", dst, n), n, self._stream()))
+
+    def compact(self, n_rows, n_keep, rows=None, seqs=None):
+        """Of the last n_rows[i] tokens the n_keep[i] listed ones (rows [n, most]) stay, moved to the front of them."""
+        n = n_rows.numel()
+        if rows is not None and (rows.dim() != 2 or rows.shape[0] != n):
+            raise ValueError("rows is [sequences, most kept rows]")
+        self._ck(self.L.redrafter_pages_compact(self.h, self._list("seqs", seqs, n), self._list("n_rows", n_rows),
+                                                self._list("n_keep", n_keep, n), self._list("rows", rows),
+                                                0 if rows is None else rows.shape[1], n, self._stream()))
+
+    def trim(self, window, sinks=0, seqs=None):
+        n = self.max_seqs if seqs is None else seqs.numel()
+        self._ck(self.L.redrafter_pages_trim(self.h, self._list("seqs", seqs), window, sinks, n, self._stream()))
+
+    def free(self, seqs=None):
+        n = self.max_seqs if seqs is None else seqs.numel()
+        self._ck(self.L.redrafter_pages_free(self.h, self._list("seqs", seqs), n, self._stream()))
+
+    def _rows(self, name, t, heads):
+        """Pointer and row stride of rows [n, heads, head_dim] whose heads lie one behind the other."""
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.dtype != self.dtype or t.device != self.device:
+            raise ValueError(f"{name}: expected rows [n, {heads}, {self.head_dim}] of {self.dtype} on {self.device}")
+        row, head, one = t.stride()
+        if (one != 1 or (head != self.head_dim and heads > 1)) and t.numel():
+            raise ValueError(f"{name}: the heads of a row have to lie one behind the other")
+        return t.data_ptr(), row if t.shape[0] > 1 else max(row, heads * self.head_dim)
+
+    def _entries(self, rows, seqs, row_off):
+        """Number of sequences of a call and the pointers of its lists."""
+        if row_off is not None:
+            n = row_off.numel() - 1
+        else:
+            n = rows
+        return n, self._list("seqs", seqs, n), self._list("row_off", row_off)
+
+    def write(self, layer, k, v, row_off=None, seqs=None, max_rows=None):
+        """K and V [rows, kv heads, head dim] of the last tokens of sequences into their pages."""
+        n, sp, op = self._entries(k.shape[0], seqs, row_off)
+        (kp, ks), (vp, vs) = self._rows("k", k, self.n_kv_heads), self._rows("v", v, self.n_kv_heads)
+        if v.shape[0] != k.shape[0]:
+            raise ValueError("k and v have different numbers of rows")
+        self._ck(self.L.redrafter_pages_write(self.h, layer, sp, op, n, k.shape[0], kp, ks, vp, vs, self._stream()))
+
+    def attention(self, layer, q, out=None, row_off=None, seqs=None, max_rows=None, window=0, sinks=0, scale=0.0, lse=None):
+        """Causal attention of rows q [rows, heads, head dim], the last tokens of sequences, over their pages; returns out.
+
+        max_rows: the most rows of any sequence (with row_off; it picks the kernel).  lse: [rows, heads] fp32, filled in."""
+        rows, heads = q.shape[0], q.shape[1]
+        n, sp, op = self._entries(rows, seqs, row_off)
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        elif out.shape != q.shape:
+            raise ValueError("out and q have different shapes")
+        (qp, qs), (outp, outs) = self._rows("q", q, heads), self._rows("out", out, heads)
+        if lse is not None and (lse.dtype != torch.float32 or lse.device != self.device or not lse.is_contiguous() or lse.numel() != rows * heads):
+            raise ValueError(f"lse: expected contiguous float32 [{rows}, {heads}] on {self.device}")
+        self._ck(self.L.redrafter_pages_attention(self.h, layer, sp, op, n, rows, (max_rows or 0) if row_off is not None else 1, heads, qp, qs,
+                                                  outp, outs, None if lse is None else lse.data_ptr(), scale, window, sinks, self._stream()))
+        return out
+
+    def poll(self):
+        self._ck(self.L.redrafter_pages_poll(self.h, self._stream()))
+
+    def launch_count(self):
+        return int(self.L.redrafter_pages_launch_count(self.h))
+
+
+def token_logprobs(logits, tokens=None, top=0, temperature=1.0, rows=None, entropy=True):
+    """Per row of logits [n, vocab] (or per entry of rows, which names rows of them): the given token's log probability, the
+    entropy, and the `top` most likely tokens.  Returns a dict of logprob, entropy, top_ids and top_logprobs."""
+    if not logits.is_cuda:
+        raise RuntimeError("token_logprobs needs a CUDA device; there is no CPU path")
+    if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError("logits is [rows, vocab] with a row's elements one behind the other")
+    dev = logits.device
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"logits lie on {dev}, which is not the current device")
+    n = logits.shape[0] if rows is None else rows.numel()
+    for name, t in (("tokens", tokens), ("rows", rows)):
+        if t is not None and (t.dtype != torch.int32 or t.device != dev or not t.is_contiguous() or t.numel() != n):
+            raise ValueError(f"{name}: expected {n} contiguous int32 on {dev}")
+    got = {}
+    if tokens is not None:
+        got["logprob"] = torch.empty(n, dtype=torch.float32, device=dev)
+    if entropy:
+        got["entropy"] = torch.empty(n, dtype=torch.float32, device=dev)
+    if top > 0:
+        got["top_ids"] = torch.empty(n, top, dtype=torch.int32, device=dev)
+        got["top_logprobs"] = torch.empty(n, top, dtype=torch.float32, device=dev)
+    ptr = {k: t.data_ptr() for k, t in got.items()}
+    a = RdLogprobs(C.sizeof(RdLogprobs), RD_DTYPE[_dtype_name(logits)], n, logits.shape[0], logits.shape[1], top, temperature, 0,
+                   logits.stride(0) if logits.shape[0] > 1 else max(logits.stride(0), logits.shape[1]), logits.data_ptr(),
+                   None if rows is None else rows.data_ptr(), None if tokens is None else tokens.data_ptr(), ptr.get("logprob"),
+                   ptr.get("entropy"), ptr.get("top_ids"), ptr.get("top_logprobs"))
+    L = lib()
+    rc = L.redrafter_token_logprobs(C.byref(a), torch.cuda.current_stream().cuda_stream)
+    if rc:
+        raise RdError(rc, L.redrafter_token_logprobs_error().decode())
+    return got

@@ -1,0 +1,336 @@
+// Log probabilities of given tokens with the distribution's entropy and its most likely tokens, one pass over the logits.
+//
+//   y_v = x_v / T,  lse = log sum_v exp(y_v),  logprob = y_t - lse,  entropy = lse - sum_v p_v y_v,  p_v = exp(y_v - lse)
+//
+// A row is one cluster of 1 to 8 CTAs whose threads take its 16-byte pieces in turn.  Each thread keeps, in 32 bits, the
+// running maximum r of x and, with d = (x - r) log2(e) / T, s = sum 2^d and u = sum 2^d d, from which logprob = (x_t - r) / T -
+// log s and entropy = log s - ln 2 u / s; they are joined over the lanes, warps and CTAs in a fixed order.  (The difference
+// x - r is formed first: it is exact where it matters, so that no log probability comes out above 0.)
+//
+// The most likely tokens (larger logit first, lower index first among equals) need no second pass over the row: the k-th
+// largest of the maxima of 128 groups of threads is a bound that at least k elements reach and, in expectation, few more
+// (k + k^2 / 256 or so); only threads whose own maximum reaches it read their pieces again (from the L2) and list what
+// reaches the bound, and the list is ranked by counting.  Rows with NaN or +inf, and lists that overflow, take one maximum
+// after another instead.
+#include <cooperative_groups.h>
+
+#include "logprobs.cuh"
+#include "pdl.cuh"
+#include "rd_internal.cuh"
+
+namespace rd {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int LP_THREADS = 512, LP_WARPS = LP_THREADS / 32, LP_GROUPS = LP_THREADS / 4, LP_LIST = 2048;
+typedef unsigned long long u64;
+
+// Order of the tokens as one number: larger logit first (NaN above all, as sorting puts it), lower index first.
+__device__ __forceinline__ u64 rank_key(float x, uint32_t index) {
+  uint32_t u = __float_as_uint(x + 0.f);   // (-0 is 0)
+  u = x != x ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
+  return ((u64)u << 32) | (0xffffffffu - index);
+}
+__device__ __forceinline__ float key_logit(u64 key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return __uint_as_float(u == 0xffffffffu ? 0x7fffffffu : (u & 0x80000000u) ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ uint32_t key_index(u64 key) { return 0xffffffffu - (uint32_t)key; }
+
+template <typename T> struct Pieces;   // 16 bytes as floats
+template <> struct Pieces<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(const uint4& v, float* x) {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+};
+template <> struct Pieces<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void unpack(const uint4& v, float* x) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+};
+
+// r: largest x so far, s and u relative to it.
+struct Sums { float r, s, u; };
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ Sums rebase(const Sums& a, float r, float c2) {
+  if (a.r == r || a.r == -INFINITY) return Sums{r, a.s, a.u};   // (nothing but -inf so far: s and u are zero, or NaN)
+  const float d = (a.r - r) * c2, c = ex2(d);
+  return Sums{r, a.s * c, c == 0.f ? 0.f * a.s : c * fmaf(a.s, d, a.u)};
+}
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c2) {
+  const float r = fmaxf(a.r, b.r);
+  const Sums x = rebase(a, r, c2), y = rebase(b, r, c2);
+  return Sums{r, x.s + y.s, x.u + y.u};
+}
+
+template <int N> __device__ __forceinline__ void add_values(Sums& a, const float (&x)[N], float c2) {
+  float m = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+  if (m > a.r) a = rebase(a, m, c2);
+  const float ref = a.r == -INFINITY ? 0.f : a.r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = (x[i] - ref) * c2, e = ex2(d);
+    a.s += e;
+    a.u = fmaf(e, fmaxf(d, -1024.f), a.u);   // (2^-1024 is zero, and 0 * -inf would not be)
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
+  pdl_enter();
+  using P = Pieces<T>;
+  constexpr int N = P::N, UNROLL = 4;
+  __shared__ u64 s_best[LP_GROUPS];
+  __shared__ u64 s_list[LP_LIST];
+  __shared__ u64 s_top[LOGPROB_MAX_TOP];
+  __shared__ Sums s_sums[LP_WARPS];
+  __shared__ Sums s_total;
+  __shared__ u64 s_bound;
+  __shared__ int s_count;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int S = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+  const int row = blockIdx.x / S, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int at = a.row_index ? a.row_index[row] : row;
+  const float nan = __uint_as_float(0x7fffffffu);
+  if (at < 0 || at >= a.n_logit_rows) {   // (the whole cluster)
+    if (part == 0) {
+      if (t == 0 && a.logprob) a.logprob[row] = nan;
+      if (t == 0 && a.entropy) a.entropy[row] = nan;
+      for (int k = t; k < a.top; k += LP_THREADS) {
+        a.top_ids[(size_t)row * a.top + k] = -1;
+        a.top_logprobs[(size_t)row * a.top + k] = nan;
+      }
+    }
+    return;
+  }
+  const T* x = reinterpret_cast<const T*>(a.logits) + (long long)at * a.row_stride;
+  const float c2 = a.inv_t * 1.4426950408889634f;
+  float x_token = nan;
+  if (part == 0 && t == 0) {
+    s_count = 0;
+    if (a.tokens && a.logprob) {
+      const int tok = a.tokens[row];
+      if ((unsigned)tok < (unsigned)a.vocab) x_token = to_f<T>(x[tok]);
+    }
+  } else if (t == 0) {
+    s_count = 0;
+  }
+  // the row's elements: single ones up to a 16-byte boundary (head), pieces, single ones behind the last piece
+  const int head = min((int)(((16 - ((uintptr_t)x & 15)) & 15) / sizeof(T)), a.vocab);
+  const int pieces = (a.vocab - head) / N, tail0 = head + pieces * N;
+  const uint4* body = reinterpret_cast<const uint4*>(x + head);
+  const int single = part == 0 ? (t < head ? t : t - head < a.vocab - tail0 ? tail0 + t - head : -1) : -1;   // this thread's single element
+  const int step = S * LP_THREADS, p0 = part * LP_THREADS + t;
+  Sums sum{-INFINITY, 0.f, 0.f};
+  float best = -INFINITY;
+  int best_at = -1;
+  auto see = [&](float v, int index) {
+    if (v > best || best_at < 0) { best = v; best_at = index; }
+  };
+  for (int p = p0; p < pieces; p += UNROLL * step) {
+    uint4 raw[UNROLL];
+#pragma unroll
+    for (int k = 0; k < UNROLL; ++k)
+      if (p + k * step < pieces) raw[k] = body[p + k * step];
+#pragma unroll
+    for (int k = 0; k < UNROLL; ++k)
+      if (p + k * step < pieces) {
+        float v[N];
+        P::unpack(raw[k], v);
+        add_values(sum, v, c2);
+#pragma unroll
+        for (int j = 0; j < N; ++j) see(v[j], head + (p + k * step) * N + j);
+      }
+  }
+  if (single >= 0) {
+    const float v[1] = {to_f<T>(x[single])};
+    add_values(sum, v, c2);
+    if (single < head ? !(best > v[0]) : v[0] > best || best_at < 0) { best = v[0]; best_at = single; }
+  }
+  const u64 mine = best_at >= 0 ? rank_key(best, (uint32_t)best_at) : 0ull;
+  // ---- the CTA's sums and the maxima of its groups of four threads
+#pragma unroll
+  for (int w = 1; w < 32; w <<= 1) {
+    const Sums o{__shfl_xor_sync(0xffffffffu, sum.r, w), __shfl_xor_sync(0xffffffffu, sum.s, w), __shfl_xor_sync(0xffffffffu, sum.u, w)};
+    sum = join(sum, o, c2);
+  }
+  if (lane == 0) s_sums[warp] = sum;
+  if (a.top) {
+    u64 g = mine;
+#pragma unroll
+    for (int w = 1; w < 4; w <<= 1) {
+      const u64 o = __shfl_xor_sync(0xffffffffu, g, w);
+      g = o > g ? o : g;
+    }
+    if ((lane & 3) == 0) s_best[t >> 2] = g;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    Sums q = lane < LP_WARPS ? s_sums[lane] : Sums{-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int w = 1; w < LP_WARPS; w <<= 1) {
+      const Sums o{__shfl_xor_sync(0xffffffffu, q.r, w), __shfl_xor_sync(0xffffffffu, q.s, w), __shfl_xor_sync(0xffffffffu, q.u, w)};
+      q = join(q, o, c2);
+    }
+    if (lane == 0) s_total = q;
+  }
+  if (a.top && t < LP_GROUPS) {   // the group maximum that top - 1 others exceed (equal ones are empty groups)
+    const u64 g = s_best[t];
+    int above = 0, equal_before = 0;
+#pragma unroll 8
+    for (int j = 0; j < LP_GROUPS; ++j) {
+      const u64 o = s_best[j];
+      above += o > g;
+      equal_before += o == g && j < t;
+    }
+    if (above + equal_before == a.top - 1) s_bound = g;
+  }
+  __syncthreads();
+  if (a.top) {
+    const float total = s_total.s;
+    bool rounds = total != total;
+    if (!rounds) {
+      const u64 bound = s_bound;
+      auto offer = [&](float v, int index) {
+        const u64 key = rank_key(v, (uint32_t)index);
+        if (key >= bound) {
+          const int place = atomicAdd(&s_count, 1);
+          if (place < LP_LIST) s_list[place] = key;
+        }
+      };
+      if (mine >= bound && mine) {
+        for (int p = p0; p < pieces; p += UNROLL * step) {
+          uint4 raw[UNROLL];
+#pragma unroll
+          for (int k = 0; k < UNROLL; ++k)
+            if (p + k * step < pieces) raw[k] = body[p + k * step];
+#pragma unroll
+          for (int k = 0; k < UNROLL; ++k)
+            if (p + k * step < pieces) {
+              float v[N];
+              P::unpack(raw[k], v);
+#pragma unroll
+              for (int j = 0; j < N; ++j) offer(v[j], head + (p + k * step) * N + j);
+            }
+        }
+        if (single >= 0) offer(to_f<T>(x[single]), single);
+      }
+      __syncthreads();
+      rounds = s_count > LP_LIST;
+    }
+    if (rounds) {   // one maximum after another, each below the one before
+      u64 before = ~0ull;
+      for (int r = 0; r < a.top; ++r) {
+        u64 m = 0;
+        auto look = [&](float v, int index) {
+          const u64 key = rank_key(v, (uint32_t)index);
+          if (key < before && key > m) m = key;
+        };
+        for (int p = p0; p < pieces; p += step) {
+          float v[N];
+          P::unpack(body[p], v);
+          for (int j = 0; j < N; ++j) look(v[j], head + p * N + j);
+        }
+        if (single >= 0) look(to_f<T>(x[single]), single);
+#pragma unroll
+        for (int w = 1; w < 32; w <<= 1) {
+          const u64 o = __shfl_xor_sync(0xffffffffu, m, w);
+          m = o > m ? o : m;
+        }
+        __syncthreads();
+        if (lane == 0) s_best[warp] = m;
+        __syncthreads();
+        m = 0;
+        for (int w = 0; w < LP_WARPS; ++w) m = s_best[w] > m ? s_best[w] : m;
+        if (t == 0) s_top[r] = m;
+        before = m;
+        if (m == 0) before = 1;   // nothing left: zeros follow
+      }
+      __syncthreads();
+    } else {
+      const int n = s_count;
+      for (int k = t; k < a.top; k += LP_THREADS) if (k >= n) s_top[k] = 0;   // fewer elements than asked for in this CTA's share
+      for (int e = t; e < n; e += LP_THREADS) {
+        const u64 key = s_list[e];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += s_list[j] > key;
+        if (above < a.top) s_top[above] = key;
+      }
+      __syncthreads();
+    }
+  }
+  // ---- over the cluster's CTAs
+  if (S > 1) {
+    cluster.sync();
+    if (part == 0) {
+      if (t == 0) {
+        Sums q = s_total;
+        for (int c = 1; c < S; ++c) q = join(q, *cluster.map_shared_rank(&s_total, c), c2);
+        s_sums[0] = q;
+      }
+      if (a.top) {
+        const int n = S * a.top;   // <= LP_LIST
+        for (int e = t; e < n; e += LP_THREADS) s_list[e] = *cluster.map_shared_rank(&s_top[e % a.top], e / a.top);
+        __syncthreads();
+        for (int e = t; e < n; e += LP_THREADS) {
+          const u64 key = s_list[e];
+          if (!key) continue;
+          int above = 0;
+          for (int j = 0; j < n; ++j) above += s_list[j] > key;
+          if (above < a.top) s_best[above] = key;   // (top <= LP_GROUPS)
+        }
+      }
+      __syncthreads();
+    }
+    cluster.sync();   // the others' shared memory has been read
+    if (part != 0) return;
+  }
+  const Sums q = S > 1 ? s_sums[0] : s_total;
+  const u64* top = S > 1 ? s_best : s_top;
+  const float ln2 = 0.6931471805599453f, ref = q.r == -INFINITY ? 0.f : q.r;
+  const float log_s = logf(q.s);
+  if (t == 0 && a.logprob) a.logprob[row] = (x_token - ref) * a.inv_t - log_s;
+  if (t == 0 && a.entropy) a.entropy[row] = log_s - q.u / q.s * ln2;
+  for (int k = t; k < a.top; k += LP_THREADS) {
+    const u64 key = top[k];
+    a.top_ids[(size_t)row * a.top + k] = (int32_t)key_index(key);
+    a.top_logprobs[(size_t)row * a.top + k] = (key_logit(key) - ref) * a.inv_t - log_s;
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_logprobs(int dtype, const LogprobArgs& a, cudaStream_t st) {
+  // CTAs per row: enough to fill the SMs when there are few rows
+  int S = 1;
+  while (S < 8 && (long long)a.rows * S < 2 * 148 && a.vocab / (2 * S) >= LP_THREADS * 4) S *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)a.rows * S);
+  cfg.blockDim = LP_THREADS;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = S; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cudaError_t e = dtype == RD_DTYPE_FP32 ? cudaLaunchKernelEx(&cfg, logprob_kernel<float>, a) : cudaLaunchKernelEx(&cfg, logprob_kernel<__nv_bfloat16>, a);
+  return e ? e : cudaGetLastError();
+}
+
+}  // namespace rd

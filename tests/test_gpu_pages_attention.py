@@ -1,0 +1,299 @@
+"""Attention over a cache in pages against 64 bits: single tokens and runs of rows, windows and sinks, lengths and sizes where
+tiles end, anything at all in places that a row does not see."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from helpers import dev
+from pages_model import attend, tolerance
+from paper_2403_09919_b200 import binding
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def build(lens, rows, heads, kv_heads, head_dim, page, dtype, seed=0, layers=1, scale=1.0, spread=1.0):
+    """A cache of sequences of these lengths whose pages lie in any order, and rows q, k, v of the last tokens (already written).
+    What no token fills is NaN."""
+    rng, gen = np.random.default_rng(seed), torch.Generator("cuda:0").manual_seed(seed)
+    held = [-(-n // page) for n in lens]
+    n_pages, S = sum(held) + 3, len(lens)
+    cache = binding.PagedCache.empty(layers, kv_heads, head_dim, page, n_pages, S, max(max(held), 1) + 1, dtype)
+    order = rng.permutation(n_pages)
+    table, at = np.full((S, max(max(held), 1) + 1), -1), 0
+    for s, n in enumerate(held):
+        table[s, :n] = order[at:at + n]
+        at += n
+    cache.page_table.copy_(dev(table))
+    cache.lens.copy_(dev(np.array(lens)))
+    cache.refs[torch.from_numpy(order[:at]).to("cuda:0")] = 1
+    cache.pool.fill_(math.nan)
+    keys, values = [], []
+    for s, n in enumerate(lens):
+        k, v = ((torch.randn(n, kv_heads, head_dim, generator=gen, device="cuda:0") * spread).to(DT[dtype]) for _ in range(2))
+        put(cache, table, s, 0, k, v, layers - 1)
+        keys.append(k)
+        values.append(v)
+    q = (torch.randn(sum(rows), heads, head_dim, generator=gen, device="cuda:0") * scale).to(DT[dtype])
+    return cache, table, q, keys, values
+
+
+def put(cache, table, s, first, k, v, layer):
+    pos = torch.arange(first, first + k.shape[0], device="cuda:0")
+    pages = torch.from_numpy(table[s]).to("cuda:0")[pos // cache.page_size]
+    cache.pool[layer, 0][pages, :, pos % cache.page_size] = k
+    cache.pool[layer, 1][pages, :, pos % cache.page_size] = v
+
+
+def compare(got, lse, q, keys, values, lens, rows, window, sinks, scale=None):
+    at = 0
+    for n, m, k, v in zip(lens, rows, keys, values):
+        part = slice(at, at + m)
+        at += m
+        if not m:
+            continue
+        ref, ref_lse, absv, absqk = attend(q[part], k, v, np.arange(n - m, n), window, sinks, scale)
+        sc = scale or 1 / math.sqrt(q.shape[-1])
+        err = (got[part].double() - ref).abs()
+        tol = tolerance(q.dtype, ref, absv, absqk, n, sc)
+        assert torch.isfinite(got[part]).all()
+        assert (err <= tol).all(), (n, m, float((err / tol).max()))
+        if lse is not None:
+            there = torch.isfinite(ref_lse)
+            assert torch.equal(there, torch.isfinite(lse[part]))
+            d = (lse[part].double() - ref_lse)[there].abs()
+            bound = ((q.shape[-1] + 8) * 2.0 ** -24 * absqk * sc + (n + 16) * 2.0 ** -24 + 2.0 ** -19 + ref_lse.abs() * 2.0 ** -22)[there]
+            assert (d <= bound).all(), float((d / bound).max())
+
+
+def run(lens, rows, heads, kv_heads, head_dim, page, dtype, window=0, sinks=0, seed=0, scale=None, spread=1.0, qscale=1.0, several=True):
+    cache, table, q, keys, values = build(lens, rows, heads, kv_heads, head_dim, page, dtype, seed, scale=qscale, spread=spread)
+    lse = torch.full((q.shape[0], heads), 7.0, device="cuda:0")
+    kw = dict(row_off=dev(np.concatenate([[0], np.cumsum(rows)])), max_rows=max(max(rows), 1)) if several else {}
+    got = cache.attention(0, q, window=window, sinks=sinks, lse=lse, scale=scale or 0.0, **kw)
+    cache.poll()
+    compare(got, lse, q, keys, values, lens, rows, window, sinks, scale)
+
+
+HEADS = [(4, 4, 64), (32, 8, 128), (16, 1, 128), (3, 3, 128), (40, 2, 64), (24, 1, 128)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,head_dim", HEADS)
+@pytest.mark.parametrize("page,window,sinks", [(16, 0, 0), (64, 0, 0), (32, 70, 5), (128, 33, 0)])
+def test_single_tokens(dtype, heads, kv_heads, head_dim, page, window, sinks):
+    lens = [1, 16, 17, 64, 63, 200, 129, 513, 2, 1000, 0]
+    run(lens, [1] * len(lens), heads, kv_heads, head_dim, page, dtype, window, sinks, seed=page, several=False)
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("lens", [[9000], [7, 30000, 1, 5000], [1] * 300, list(range(1, 130))])
+def test_single_tokens_of_long_and_of_many_sequences(page, lens):
+    run(lens, [1] * len(lens), 8, 2, 128, page, "bf16", seed=len(lens), several=False)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 200), (64, 64), (100, 3), (5000, 4), (128, 1), (129, 0)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_windows_of_single_tokens(dtype, window, sinks):
+    lens = [1, 2, 16, 63, 64, 65, 100, 128, 129, 130, 400, 1025]
+    run(lens, [1] * len(lens), 4, 2, 128, 32, dtype, window, sinks, several=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(4, 4, 128), (8, 2, 128), (3, 3, 64)])
+@pytest.mark.parametrize("page,window,sinks", [(16, 0, 0), (128, 0, 0), (32, 100, 5), (64, 17, 0), (64, 130, 140)])
+def test_runs_of_rows(dtype, heads, kv_heads, head_dim, page, window, sinks):
+    lens, rows = [300, 128, 129, 1, 700, 40, 555], [300, 128, 1, 1, 257, 0, 33]
+    run(lens, rows, heads, kv_heads, head_dim, page, dtype, window, sinks, seed=page)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (256, 4), (1000, 0)])
+def test_a_long_run_of_rows(window, sinks):
+    run([2500, 1300], [2100, 1300], 2, 1, 128, 64, "bf16", window, sinks)
+
+
+@pytest.mark.parametrize("several", [False, True])
+def test_scores_far_apart_and_a_scale(several):
+    """Scores in the hundreds, of either sign: maxima move by large steps, weights are 0 and 1."""
+    lens, rows = [700, 300], ([1, 1] if not several else [200, 150])
+    run(lens, rows, 4, 2, 128, 32, "bf16", seed=3, qscale=30.0, several=several)
+    run(lens, rows, 4, 2, 128, 32, "bf16", seed=4, scale=0.5, several=several)
+    run(lens, rows, 4, 2, 128, 32, "bf16", window=90, sinks=2, seed=5, qscale=30.0, several=several)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf, 3.3e38])
+@pytest.mark.parametrize("dtype,head_dim", [("bf16", 128), ("fp32", 128), ("bf16", 64)])
+def test_what_a_row_does_not_see_does_not_reach_it(bad, dtype, head_dim):
+    """Keys and values outside a window hold NaN, infinities or the type's largest numbers; some rows of a call see them and
+    the rows behind do not."""
+    window, sinks, page = 40, 3, 32
+    lens, rows = [400, 150], [90, 60]
+    for single in (True, False):
+        r = [1, 1] if single else rows
+        cache, table, q, keys, values = build(lens, r, 4, 2, head_dim, page, dtype, seed=9)
+        spots = [(0, 3, 200), (1, 3, 50)] if single else [(0, 3, 230), (1, 3, 30), (0, 320, 322)]
+        for s, a, b in spots:
+            for x in (keys[s], values[s]):
+                x[a:b] = bad
+            put(cache, table, s, 0, keys[s], values[s], 0)
+        kw = {} if single else dict(row_off=dev(np.array([0, 90, 150])), max_rows=90)
+        got = cache.attention(0, q, window=window, sinks=sinks, **kw)
+        cache.poll()
+        at = 0
+        for s, (n, m) in enumerate(zip(lens, r)):
+            pos = np.arange(n - m, n)
+            clean = np.array([not any(max(a, p - window + 1) < min(b, p + 1) for (t, a, b) in spots if t == s) for p in pos])
+            assert clean.any()
+            idx = torch.from_numpy(np.nonzero(clean)[0]).to("cuda:0")
+            qs = q[at:at + m][idx]
+            ref, _, absv, absqk = attend(qs, keys[s], values[s], pos[clean], window, sinks)
+            err = (got[at:at + m][idx].double() - ref).abs()
+            assert (err <= tolerance(q.dtype, ref, absv, absqk, n, 1 / math.sqrt(head_dim))).all()
+            if not np.isfinite(bad) and not clean.all():      # and where it is seen it does
+                dirty = torch.from_numpy(np.nonzero(~clean)[0]).to("cuda:0")
+                assert not torch.isfinite(got[at:at + m][dirty]).all()
+            at += m
+
+
+def test_rows_behind_the_last_sequence_stay():
+    for dtype, hd in (("bf16", 128), ("fp32", 64)):
+        cache, table, q, keys, values = build([200, 90], [60, 50], 4, 2, hd, 16, dtype)
+        q = torch.cat([q, torch.full((40, 4, hd), math.nan, device="cuda:0", dtype=q.dtype)])
+        out, lse = torch.full_like(q, 5.0), torch.full((150, 4), 5.0, device="cuda:0")
+        cache.attention(0, q, out=out, lse=lse, row_off=dev(np.array([0, 60, 110])), max_rows=60)
+        cache.poll()
+        assert (out[110:] == 5).all() and (lse[110:] == 5).all()
+        compare(out, lse, q, keys, values, [200, 90], [60, 50], 0, 0)
+
+
+def test_strides_layers_lists_and_in_one_buffer():
+    """Rows of q, k and v as parts of one projection's output, a list of sequences in any order (one of them twice), the last of
+    several layers."""
+    heads, kv, hd, page = 8, 2, 128, 16
+    lens = [70, 33, 200]
+    for rows in ([1, 1, 1, 1], [3, 20, 50, 1]):
+        cache, table, _, keys, values = build(lens, [1, 1, 1], heads, kv, hd, page, "bf16", layers=3)
+        seqs = [2, 0, 1, 2]
+        total = sum(rows)
+        fused = torch.randn(total, heads + 2 * kv, hd, device="cuda:0").to(torch.bfloat16)
+        q = fused[:, :heads]
+        out = torch.zeros(total, heads + 3, hd, device="cuda:0", dtype=torch.bfloat16)
+        kw = dict(seqs=dev(np.array(seqs)))
+        if total > 4:
+            kw.update(row_off=dev(np.concatenate([[0], np.cumsum(rows)])), max_rows=max(rows))
+        cache.attention(2, q, out=out[:, 2:2 + heads], **kw)
+        cache.poll()
+        at = 0
+        for s, m in zip(seqs, rows):
+            compare(out[at:at + m, 2:2 + heads], None, q[at:at + m], [keys[s]], [values[s]], [lens[s]], [m], 0, 0)
+            at += m
+        assert (out[:, :2] == 0).all() and (out[:, 2 + heads:] == 0).all()
+
+
+def test_pages_out_of_the_pool_and_trimmed_ones():
+    for rows in ([1, 1], [80, 80]):
+        cache, table, q, keys, values = build([400, 400], rows, 4, 2, 128, 16, "bf16")
+        kw = dict(row_off=dev(np.array([0, rows[0], sum(rows)])), max_rows=max(rows)) if rows[0] > 1 else {}
+        want = cache.attention(0, q, window=50, sinks=3, **kw)
+        cache.poll()
+        cache.page_table[:, 1:(400 - rows[0] - 50) // 16] = -1          # what the window has left behind
+        again = cache.attention(0, q, window=50, sinks=3, **kw)
+        cache.poll()
+        assert torch.equal(want, again)
+        cache.page_table[0, 24] = 1 << 30                               # a key that is seen lies nowhere: reported
+        got = cache.attention(0, q, window=50, sinks=3, **kw)
+        with pytest.raises(binding.RdError) as e:
+            cache.poll()
+        assert e.value.code == 1
+        assert torch.equal(got[rows[0]:], want[rows[0]:])               # and the other sequence is as it was
+
+
+def test_a_sequence_outside_the_table_and_more_rows_than_announced():
+    cache, table, q, keys, values = build([100, 50], [1, 1], 4, 2, 128, 16, "bf16")
+    out = cache.attention(0, q, seqs=dev(np.array([9, 1])))
+    with pytest.raises(binding.RdError):
+        cache.poll()
+    assert (out[0] == 0).all()
+    compare(out[1:], None, q[1:], keys[1:], values[1:], [50], [1], 0, 0)
+    q3 = torch.cat([q, q])
+    for limit in (1, 2):
+        out = torch.full_like(q3, 3.0)
+        cache.attention(0, q3, out=out, row_off=dev(np.array([0, 3, 4])), max_rows=limit)
+        with pytest.raises(binding.RdError):
+            cache.poll()
+        assert (out[:3] == 3).all()
+        compare(out[3:], None, q3[3:], keys[1:], values[1:], [50], [1], 0, 0)
+
+
+def test_more_rows_than_tokens():
+    """Rows that would lie before a sequence's first token have no keys."""
+    cache, table, q, keys, values = build([5], [9], 4, 2, 128, 16, "bf16")
+    lse = torch.zeros(9, 4, device="cuda:0")
+    out = cache.attention(0, q, row_off=dev(np.array([0, 9])), max_rows=9, lse=lse)
+    cache.poll()
+    assert (out[:4] == 0).all() and (lse[:4] == -math.inf).all()
+    compare(out[4:], lse[4:], q[4:], keys, values, [5], [5], 0, 0)
+
+
+def test_in_graphs_and_repeated():
+    """Captured calls of two sizes share the handle's workspace in one stream; every replay gives the same bits."""
+    lens = [3000, 50, 700]
+    cache, table, q, keys, values = build(lens, [1, 1, 1], 8, 2, 128, 32, "bf16")
+    rows = [100, 50, 300]
+    q2 = torch.randn(450, 8, 128, device="cuda:0").to(torch.bfloat16)
+    off = dev(np.concatenate([[0], np.cumsum(rows)]))
+    want = cache.attention(0, q).clone(), cache.attention(0, q2, row_off=off, max_rows=300, window=64, sinks=2).clone()
+    o1, o2 = torch.empty_like(q), torch.empty_like(q2)
+    torch.cuda.synchronize()
+    g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g1):
+        cache.attention(0, q, out=o1)
+    with torch.cuda.graph(g2):
+        cache.attention(0, q2, out=o2, row_off=off, max_rows=300, window=64, sinks=2)
+        cache.attention(0, q, out=o1)
+    for _ in range(3):
+        o1.zero_(), o2.zero_()
+        g1.replay()
+        assert torch.equal(o1, want[0])
+        o1.zero_()
+        g2.replay()
+        g1.replay()
+        assert torch.equal(o1, want[0]) and torch.equal(o2, want[1])
+    cache.poll()
+
+
+def test_refusals():
+    cache, table, q, keys, values = build([50], [1], 4, 2, 128, 16, "bf16")
+
+    def refused(code, **kw):
+        with pytest.raises(binding.RdError) as e:
+            cache.attention(kw.pop("layer", 0), kw.pop("q", q), **kw)
+        assert e.value.code == code
+
+    refused(1, layer=1)
+    refused(1, layer=-1)
+    refused(1, window=-1)
+    refused(1, sinks=-1)
+    refused(1, scale=-1.0)
+    refused(1, scale=math.nan)
+    refused(2, q=torch.cat([q, q[:, :1]], 1))                      # five heads on two
+    buf = torch.zeros(4 * 128 + 8, device="cuda:0", dtype=torch.bfloat16)
+    refused(2, q=buf[1:513].view(1, 4, 128))                       # not on a 16-byte boundary
+    with pytest.raises(ValueError):
+        cache.attention(0, q.float())
+    with pytest.raises(ValueError):
+        cache.attention(0, q.transpose(1, 2))
+    with pytest.raises(ValueError):
+        cache.attention(0, q, out=q[:, :2])
+    with pytest.raises(ValueError):
+        cache.attention(0, q, row_off=torch.zeros(2, dtype=torch.int64, device="cuda:0"))
+    with pytest.raises(ValueError):
+        cache.attention(0, q, lse=torch.zeros(1, 4, device="cuda:0", dtype=torch.float64))
+    assert cache.attention(0, q[:0]).shape == (0, 4, 128)
+    n = cache.launch_count()
+    with pytest.raises(binding.RdError):
+        cache.write(1, keys[0][:1], values[0][:1])
+    assert cache.launch_count() == n
+    cache.poll()
