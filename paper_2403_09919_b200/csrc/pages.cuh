@@ -69,6 +69,10 @@ struct PageAttention {
   int heads, layer, window, sinks;   // window 0: every earlier key
   float scale;
 };
+// one token per sequence, bf16
+size_t pages_token_part_bytes(const PageView& pv, int grid);
+cudaError_t pages_token_prepare(int hd);
+cudaError_t launch_pages_token(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int grid, cudaStream_t st);
 cudaError_t launch_pages_attention_plain(const PageView& pv, int dtype, const PageRows& rows, const PageAttention& a, cudaStream_t st);
 
 }  // namespace rd

@@ -12,10 +12,20 @@
 
 using namespace rd;
 
+namespace {
+struct alignas(64) MapBox {   // opaque storage of one CUtensorMap
+  unsigned char bytes[128];
+};
+constexpr int TOKEN_MAX_GRID = 160;   // upper bound of the SM count that the parts are sized for
+}  // namespace
+
 struct rd_pages {
+  MapBox map_parts;   // the pool's rows, min(page_size, 64) to a box (bf16)
   PageView pv;
   int dtype, device;
   int32_t* scratch;
+  char* parts;      // joins of the attention kernel for single tokens (bf16)
+  int grid;         // SMs
   int64_t launches;
   char err[256];
 };
@@ -72,7 +82,8 @@ bool view_shape_ok(const PageView& pv) {
   return true;
 }
 
-size_t page_workspace(const PageView& pv) { return 256 + (pages_scratch_ints(pv) * 4 + 255) / 256 * 256; }
+size_t scratch_bytes(const PageView& pv) { return (pages_scratch_ints(pv) * 4 + 255) / 256 * 256; }
+size_t page_workspace(const PageView& pv) { return 256 + scratch_bytes(pv) + (pv.es == 2 ? pages_token_part_bytes(pv, TOKEN_MAX_GRID) : 0); }
 
 // What every call on a handle checks first.
 int enter(rd_pages* h, int n) {
@@ -137,7 +148,20 @@ int redrafter_pages_init(const rd_page_cache* cache, void* workspace, size_t ws_
   h->pv = pv; h->dtype = cache->dtype; h->device = dev; h->launches = 0; h->err[0] = 0;
   h->pv.status = (int32_t*)workspace;
   h->scratch = (int32_t*)((char*)workspace + 256);
-  cudaError_t e = cudaMemsetAsync(workspace, 0, 256, 0);
+  h->parts = (char*)h->scratch + scratch_bytes(pv);
+  cudaError_t e = cudaDeviceGetAttribute(&h->grid, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess && pv.es == 2) {
+    if (h->grid > TOKEN_MAX_GRID) h->grid = TOKEN_MAX_GRID;
+    const uint64_t pool_rows = (uint64_t)pv.n_layers * 2 * pv.n_pages * pv.H * pv.ps;
+    const int rc = tc_make_map_parts(h->map_parts.bytes, pv.pool, pool_rows, pv.hd, pv.ps < 64 ? pv.ps : 64);
+    if (rc) {
+      delete h;
+      return init_fail(RD_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d for the pool", rc);
+    }
+    e = pages_token_prepare(pv.hd);
+    if (e == cudaSuccess) e = cudaMemsetAsync(h->parts, 0, pages_token_part_bytes(pv, TOKEN_MAX_GRID), 0);
+  }
+  if (e == cudaSuccess) e = cudaMemsetAsync(workspace, 0, 256, 0);
   if (e == cudaSuccess) e = launch_pages_scratch(h->pv, h->scratch, 0);
   if (e == cudaSuccess) e = cudaStreamSynchronize(0);
   if (e != cudaSuccess) {
@@ -243,12 +267,13 @@ int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, c
   const long long row = (long long)n_heads * h->pv.hd;
   if (q_stride < row || out_stride < row) return fail(h, RD_ERR_SHAPE, "row strides %lld and %lld, a row has %lld elements", (long long)q_stride, (long long)out_stride, row);
   if (!aligned16(q, q_stride, h->pv.es) || !aligned16(out, out_stride, h->pv.es)) return fail(h, RD_ERR_SHAPE, "rows of q and out have to begin on 16-byte boundaries");
-  const PageRows rows{seqs, row_off, n, n_rows, max_rows > 0 ? max_rows : n_rows};
+  const PageRows rows{seqs, row_off, n, n_rows, !row_off ? 1 : max_rows > 0 ? max_rows : n_rows};
   PageAttention a;
   a.q = q; a.out = out; a.lse = lse; a.q_stride = q_stride; a.out_stride = out_stride; a.heads = n_heads; a.layer = layer;
   a.window = window; a.sinks = window ? sinks : 0;
   a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)h->pv.hd);
-  PCK(launch_pages_attention_plain(h->pv, h->dtype, rows, a, (cudaStream_t)stream));
+  if (h->pv.es == 2 && rows.max_rows == 1) PCK(launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, (cudaStream_t)stream));
+  else PCK(launch_pages_attention_plain(h->pv, h->dtype, rows, a, (cudaStream_t)stream));
   h->launches++;
   return RD_OK;
 }
@@ -261,6 +286,8 @@ int redrafter_pages_poll(rd_pages* h, void* stream) {
   PCK(cudaStreamSynchronize(st));
   if (v == 0) return RD_OK;
   PCK(cudaMemsetAsync(h->pv.status, 0, sizeof(int32_t), st));
+  if ((v & DEV_ERR_TIMEOUT) && h->pv.es == 2)   // a launch that gave up may have left counters behind
+    PCK(cudaMemsetAsync(h->parts, 0, pages_token_part_bytes(h->pv, TOKEN_MAX_GRID), st));
   if (v & DEV_ERR_TIMEOUT) return fail(h, RD_ERR_TIMEOUT, "device status 0x%x: a bounded wait gave up", v);
   if (v & DEV_ERR_CAPACITY) return fail(h, RD_ERR_CAPACITY, "device status 0x%x: too few free pages, a call that extends changed nothing", v);
   return fail(h, RD_ERR_INVALID_ARG, "device status 0x%x: a sequence, length, row or page out of range was skipped", v);

@@ -1,0 +1,477 @@
+// Attention of one new token per sequence over a cache in pages (bf16): the keys are split evenly over the SMs and the parts
+// joined in the same launch.
+//
+//   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(scale log2(e) q . k_j - m),  m the running maximum
+//
+// The cache's stream bounds it (every visible K and V is read once, for all query heads of its key and value head), so the
+// design is about keeping that stream full whatever the lengths are:
+//   - The work is a line of units: chunks of 64 keys, for each sequence and key and value head (and, beyond 16 query heads on
+//     one of those, each 16 of them: an "item").  CTA c of G takes the units [T c / G, T (c + 1) / G), wherever sequences
+//     begin and end; the line is worked out on the device from the lengths, so nothing has to be planned on the host.
+//   - A producer warp copies chunks by TMA, a page's rows at a time, into a ring of six stages of 32 KB that runs ahead over
+//     the ends of items: while a part is joined and written, the stream goes on.
+//   - Four warps take 16 keys of every chunk each, on their own: scores by mma (16 query rows; a single token has few rows,
+//     so the tensor cores are nowhere near their rate), running maximum and sum per row, weights to bf16, V by ldmatrix.trans.
+//     What they hold is joined in shared memory at the end of an item.
+//   - An item that crosses CTAs leaves its parts (unscaled output, maximum, sum, fp32) in the workspace; the last CTA to
+//     arrive joins them in the order of the CTAs, so that the result does not depend on who is last.
+// Keys outside the row's sight are masked by selection and their V is replaced by zeros bit by bit: they may hold anything.
+#include <cuda.h>
+
+#include "pages_attention.cuh"
+#include "pdl.cuh"
+#include "tcgen05.cuh"
+
+namespace rd {
+
+namespace {
+
+constexpr int TK_KEYS = 64;          // keys of a chunk
+constexpr int TK_WARPS = 4;          // consumer warps, 16 keys each
+constexpr int TK_THREADS = TK_WARPS * 32 + 32;
+constexpr int TK_STAGES = 6;
+constexpr int TK_MIN_UNITS = 3;      // units a CTA takes at least
+
+struct TokenParams {
+  PageView pv;
+  PageRows rows;
+  PageAttention a;
+  int group, tiles;     // query heads per key and value head; tiles of 16 of them
+  float* parts;         // [grid][2][16][HD + 4]: unscaled output, maximum, sum
+  int32_t* arrived;     // [grid], zero between launches
+};
+
+// The chunks of one entry: the ones that hold sinks, then those from the window's first key on.
+struct Span {
+  int len, start, sink_end, sink_chunks, first_chunk, chunks;
+};
+
+__device__ __forceinline__ Span span_of(const TokenParams& p, int i, int* seq, int* row) {
+  Span s;
+  int first, m;
+  page_rows_of(p.rows, i, &first, &m);
+  *row = first;
+  *seq = page_seq_of(p.pv, p.rows.seqs, i);
+  s.len = *seq >= 0 ? page_len_of(p.pv, *seq) : 0;
+  visible_keys(s.len - 1, p.a.window, p.a.sinks, &s.sink_end, &s.start);
+  s.first_chunk = s.start / TK_KEYS;
+  s.sink_chunks = min((s.sink_end + TK_KEYS - 1) / TK_KEYS, s.first_chunk);
+  s.chunks = s.sink_chunks + (s.len + TK_KEYS - 1) / TK_KEYS - s.first_chunk;
+  s.chunks = m == 1 ? max(s.chunks, 1) : 0;   // (an empty sequence still writes its zeros)
+  return s;
+}
+
+// A place on the line of units.
+struct Cursor {
+  int i, item, chunk;        // entry, item of it (key and value head, tile of query heads), chunk of the item
+  int seq, row;
+  Span s;
+  long long item_begin;      // unit at which the item begins
+};
+
+__device__ __forceinline__ void next_unit(const TokenParams& p, int items, Cursor& c) {
+  if (++c.chunk < c.s.chunks) return;
+  c.chunk = 0;
+  c.item_begin += c.s.chunks;
+  if (++c.item < items) return;
+  c.item = 0;
+  do {
+    if (++c.i >= p.rows.n) { c.s.chunks = 0; return; }
+    c.s = span_of(p, c.i, &c.seq, &c.row);
+  } while (c.s.chunks == 0);
+}
+
+__device__ __forceinline__ int first_key(const Span& s, int chunk) {
+  return (chunk < s.sink_chunks ? chunk : s.first_chunk + chunk - s.sink_chunks) * TK_KEYS;
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TK_WARPS * 32) : "memory"); }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+               "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+
+template <int HD> __host__ __device__ constexpr int token_stage_bytes() { return 2 * TK_KEYS * HD * 2; }
+template <int HD> __host__ __device__ constexpr int token_pitch() { return HD + 4; }   // floats of a row of parts; also keeps the joins free of bank conflicts
+template <int HD> constexpr size_t token_smem() {
+  return 1024 + (size_t)TK_STAGES * token_stage_bytes<HD>() + (size_t)TK_WARPS * 16 * 2 * 4 + (size_t)(TK_WARPS - 1) * 16 * token_pitch<HD>() * 4 + 256;
+}
+
+// WIDE: more than 8 query heads in an item (rows 8 to 15 of the tile are in use).
+template <int HD, bool WIDE>
+__global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid_constant__ CUtensorMap map, const TokenParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  constexpr int STAGE = token_stage_bytes<HD>(), PITCH = token_pitch<HD>(), KSTEPS = HD / 16;
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - raw);
+  float* s_stat = reinterpret_cast<float*>(gen + TK_STAGES * STAGE);   // [2][TK_WARPS][16] maxima, sums
+  float* s_out = s_stat + 2 * TK_WARPS * 16;                           // [TK_WARPS - 1][16][PITCH] outputs of warps 1 ..
+  uint8_t* misc = reinterpret_cast<uint8_t*>(s_out + (TK_WARPS - 1) * 16 * PITCH);
+  const uint32_t bars = smem_u32(misc);   // full, then empty
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 16 * TK_STAGES);
+  long long* s_total = reinterpret_cast<long long*>(misc + 16 * TK_STAGES + 8);   // [1] all chunks, [1] chunks before the CTA's first entry
+  int* s_first = reinterpret_cast<int*>(s_total + 2);                             // [1] that entry, [1] whether this CTA joins
+  long long* s_scan = reinterpret_cast<long long*>(s_first + 2);                  // [TK_WARPS + 1]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const PageView& pv = p.pv;
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+    for (int s = 0; s < TK_STAGES; ++s) { mbar_init(bars + 8u * s, 1); mbar_init(bars + 8u * (TK_STAGES + s), TK_WARPS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  pdl_enter();
+
+  // ---- the line of units and this CTA's part of it
+  const int items = pv.H * p.tiles;
+  const int per = (p.rows.n + TK_THREADS - 1) / TK_THREADS, e0 = min((int)threadIdx.x * per, p.rows.n), e1 = min(e0 + per, p.rows.n);
+  long long mine = 0;
+  for (int i = e0; i < e1; ++i) {
+    int seq, row;
+    mine += span_of(p, i, &seq, &row).chunks;
+  }
+  long long before = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += v;
+  }
+  if (lane == 31) s_scan[warp] = before;
+  __syncthreads();
+  long long chunks = 0;
+  before -= mine;
+  for (int w = 0; w <= TK_WARPS; ++w) {
+    if (w < warp) before += s_scan[w];
+    chunks += s_scan[w];
+  }
+  const long long T = chunks * items;
+  const long long want = (T + TK_MIN_UNITS - 1) / TK_MIN_UNITS;
+  const int G = (int)min((long long)gridDim.x, want), c = blockIdx.x;
+  if (blockIdx.x == 0)   // entries that cannot be answered
+    for (int i = e0; i < e1; ++i) {
+      int first, m;
+      page_rows_of(p.rows, i, &first, &m);
+      if (m > 1 || (m == 1 && page_seq_of(pv, p.rows.seqs, i) < 0)) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
+    }
+  if (c >= G) return;
+  const long long u0 = T * c / G, u1 = T * (c + 1) / G;
+  const long long target = u0 / items;   // chunk count at which the CTA's first entry lies
+  if (target >= before && target < before + mine) {
+    int i = e0, seq, row;
+    long long at = before;
+    for (;; ++i) {
+      const int n = span_of(p, i, &seq, &row).chunks;
+      if (target < at + n) break;
+      at += n;
+    }
+    *s_first = i;
+    s_total[1] = at;
+  }
+  __syncthreads();
+  Cursor cur;
+  cur.i = *s_first;
+  cur.s = span_of(p, cur.i, &cur.seq, &cur.row);
+  {
+    const long long r = u0 - s_total[1] * items;
+    cur.item = (int)(r / cur.s.chunks);
+    cur.chunk = (int)(r - (long long)cur.item * cur.s.chunks);
+    cur.item_begin = u0 - cur.chunk;
+  }
+  const int n_units = (int)(u1 - u0);
+
+  const int box_rows = min(pv.ps, TK_KEYS), boxes = TK_KEYS / box_rows;
+  if (warp == TK_WARPS) {
+    // ===================== producer: lane b fetches box b of the chunk's K and V =====================
+    const long long pool_rows = (long long)pv.n_layers * 2 * pv.n_pages * pv.H * pv.ps, plane_rows = (long long)pv.n_pages * pv.H * pv.ps;
+    constexpr int NOT_WANTED = -2;
+    auto page_of = [&](const Cursor& u, int* slot) {   // page of this lane's box and the box's first token in it
+      const int k0 = first_key(u.s, u.chunk) + lane * box_rows;
+      *slot = k0 & (pv.ps - 1);
+      if (lane >= boxes || k0 >= u.s.len || u.seq < 0) return NOT_WANTED;
+      if (k0 >= u.s.sink_end && k0 + box_rows <= u.s.start) return NOT_WANTED;   // between the sinks and the window
+      const int pg = pv.table[(size_t)u.seq * pv.max_pages + (k0 >> pv.ps_log2)];
+      return (unsigned)pg < (unsigned)pv.n_pages ? pg : -1;
+    };
+    int slot, page = page_of(cur, &slot);
+    bool ok = true;
+    for (int n = 0; n < n_units; ++n) {
+      const int st = n % TK_STAGES;
+      const int h = cur.item / p.tiles, pg = page, first = slot;
+      const bool wanted = pg != NOT_WANTED;
+      if (n + 1 < n_units) {   // the next chunk's pages are looked up before this one's stage is waited for
+        next_unit(p, items, cur);
+        page = page_of(cur, &slot);
+      }
+      if (n >= TK_STAGES) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (TK_STAGES + st), ((n / TK_STAGES) & 1) ^ 1u, abort_flag, pv.status));
+      if (!ok) break;
+      const uint32_t count = __popc(__ballot_sync(0xffffffffu, wanted));
+      if (lane == 0) mbar_expect_tx(bars + 8u * st, count * (uint32_t)(2 * box_rows * HD * 2));
+      __syncwarp();
+      if (wanted) {
+        const bool there = pg >= 0;
+        if (!there) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
+        // (behind the pool's last row the copy fills in zeros)
+        const long long row = there ? (((long long)p.a.layer * 2 * pv.n_pages + pg) * pv.H + h) * pv.ps + first : pool_rows;
+        const uint32_t dst = base + (uint32_t)(st * STAGE + lane * box_rows * HD * 2);
+        tma_load_3d(dst, &map, bars + 8u * st, 0, (int)row, 0);
+        tma_load_3d(dst + STAGE / 2, &map, bars + 8u * st, 0, (int)(there ? row + plane_rows : pool_rows), 0);
+      }
+    }
+    if (!ok) {   // copies already issued land before the CTA's shared memory is given back
+      const unsigned long long t0 = now_ns();
+      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+    return;
+  }
+
+  // ===================== consumers =====================
+  const int g = lane >> 2, t4 = lane & 3;
+  const float scale2 = p.a.scale * LOG2E;
+  uint32_t q[KSTEPS][4];
+  float o[HD / 8][4];
+  float m[2], l[2];
+  // this warp's 16 keys of a chunk lie in one page
+  const int wkey = warp * 16, wbox = wkey / box_rows, wrow = wkey - wbox * box_rows;
+  const uint32_t wbase = base + (uint32_t)(wbox * box_rows * HD * 2 + wrow * 128), half_step = (uint32_t)box_rows * 128u;
+  // ldmatrix addresses: lane l gives row (l & 7) of matrix l >> 3
+  const int mat = lane >> 3, mrow = lane & 7;
+  const int krow = (mat >> 1) * 8 + mrow, kcol = mat & 1;   // K: keys 0-7 | 0-7 | 8-15 | 8-15, dimensions 0-7 | 8-15 | ...
+  const int vrow = (mat & 1) * 8 + mrow, vcol = mat >> 1;   // V: keys 0-7 | 8-15 | 0-7 | 8-15, dimensions 0-7 | 0-7 | 8-15 | 8-15
+  bool ok = true;
+  for (int n = 0; n < n_units;) {
+    const Cursor item = cur;
+    const int h = item.item / p.tiles, tile = item.item - h * p.tiles;
+    const int q_rows = min(16, p.group - tile * 16);
+    const int todo = min(item.s.chunks - item.chunk, n_units - n);
+    const long long head0 = (long long)h * p.group + tile * 16;
+    // the query rows as A fragments (zeros behind the last one)
+    {
+      const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(p.a.q) + (long long)item.row * p.a.q_stride + head0 * HD + 2 * t4;
+#pragma unroll
+      for (int k = 0; k < KSTEPS; ++k) {
+        q[k][0] = g < q_rows ? *reinterpret_cast<const uint32_t*>(src + g * HD + 16 * k) : 0u;
+        q[k][2] = g < q_rows ? *reinterpret_cast<const uint32_t*>(src + g * HD + 16 * k + 8) : 0u;
+        q[k][1] = WIDE && g + 8 < q_rows ? *reinterpret_cast<const uint32_t*>(src + (g + 8) * HD + 16 * k) : 0u;
+        q[k][3] = WIDE && g + 8 < q_rows ? *reinterpret_cast<const uint32_t*>(src + (g + 8) * HD + 16 * k + 8) : 0u;
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < HD / 8; ++d) { o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f; }
+    m[0] = m[1] = -INFINITY; l[0] = l[1] = 0.f;
+    for (int x = 0; x < todo; ++x, ++n) {
+      const int st = n % TK_STAGES;
+      const int k0 = first_key(item.s, item.chunk + x) + wkey;
+      ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * st, (n / TK_STAGES) & 1, abort_flag, pv.status));
+      if (!ok) break;
+      const uint32_t sk = wbase + (uint32_t)(st * STAGE), sv = sk + STAGE / 2;
+      // which of the 16 keys the row sees
+      uint32_t seen = 0xffffu;
+      if (k0 + 16 > item.s.len || (k0 < item.s.start && k0 + 16 > item.s.sink_end)) {
+        seen = 0;
+#pragma unroll
+        for (int b = 0; b < 16; ++b) seen |= (k0 + b < item.s.len && (k0 + b >= item.s.start || k0 + b < item.s.sink_end)) ? 1u << b : 0u;
+      }
+      if (seen) {
+        float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+          uint32_t b[4];
+          const int col = 2 * k + kcol;   // 16-byte column of the row
+          ldsm4(sk + (uint32_t)(col >> 3) * half_step + krow * 128 + (((col & 7) ^ (krow & 7)) << 4), b);
+          mma_bf16(c0, q[k], b[0], b[1]);
+          mma_bf16(c1, q[k], b[2], b[3]);
+        }
+        // keys 2 t4, 2 t4 + 1 in c0 and 8 further in c1; rows g in [0], [1] and g + 8 in [2], [3]
+        if (seen != 0xffffu) {
+          const uint32_t w = seen >> (2 * t4);
+          if (!(w & 1u)) c0[0] = c0[2] = -INFINITY;
+          if (!(w & 2u)) c0[1] = c0[3] = -INFINITY;
+          if (!(w & 256u)) c1[0] = c1[2] = -INFINITY;
+          if (!(w & 512u)) c1[1] = c1[3] = -INFINITY;
+        }
+        uint32_t pa[4];
+#pragma unroll
+        for (int r = 0; r < (WIDE ? 2 : 1); ++r) {
+          float mx = fmaxf(fmaxf(c0[2 * r], c0[2 * r + 1]), fmaxf(c1[2 * r], c1[2 * r + 1]));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+          const float m_new = fmaxf(m[r], mx * scale2);
+          const float ref = m_new == -INFINITY ? 0.f : m_new;
+          if (__any_sync(0xffffffffu, m_new != m[r])) {
+            const float corr = fast_exp2(m[r] - ref);
+            l[r] *= corr;
+#pragma unroll
+            for (int d = 0; d < HD / 8; ++d) { o[d][2 * r] *= corr; o[d][2 * r + 1] *= corr; }
+            m[r] = m_new;
+          }
+          const float p0 = fast_exp2(fmaf(c0[2 * r], scale2, -ref)), p1 = fast_exp2(fmaf(c0[2 * r + 1], scale2, -ref));
+          const float p2 = fast_exp2(fmaf(c1[2 * r], scale2, -ref)), p3 = fast_exp2(fmaf(c1[2 * r + 1], scale2, -ref));
+          l[r] += (p0 + p1) + (p2 + p3);
+          pa[r] = pack_bf16(p0, p1); pa[r + 2] = pack_bf16(p2, p3);   // (the weights' rounding: half a step of bf16 each, as in the library's other kernels)
+        }
+        if (!WIDE) pa[1] = pa[3] = 0u;
+        const uint32_t z0 = ((seen >> (2 * t4)) & 1u ? 0xffffu : 0u) | ((seen >> (2 * t4 + 1)) & 1u ? 0xffff0000u : 0u);
+        const uint32_t z1 = ((seen >> (2 * t4 + 8)) & 1u ? 0xffffu : 0u) | ((seen >> (2 * t4 + 9)) & 1u ? 0xffff0000u : 0u);
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) {
+          uint32_t b[4];
+          const int col = 2 * d + vcol;
+          ldsm4_trans(sv + (uint32_t)(col >> 3) * half_step + vrow * 128 + (((col & 7) ^ (vrow & 7)) << 4), b);
+          if (seen != 0xffffu) { b[0] &= z0; b[1] &= z1; b[2] &= z0; b[3] &= z1; }
+          mma_bf16(o[2 * d], pa, b[0], b[1]);
+          mma_bf16(o[2 * d + 1], pa, b[2], b[3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars + 8u * (TK_STAGES + st));
+    }
+    if (!ok) return;
+    // ---- join the warps: maxima and sums of all, outputs of warps 1 .. through shared memory
+    consumers_sync();   // the join before has been read
+#pragma unroll
+    for (int r = 0; r < (WIDE ? 2 : 1); ++r) {
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+      if (t4 == 0) {
+        s_stat[warp * 16 + g + 8 * r] = m[r];
+        s_stat[TK_WARPS * 16 + warp * 16 + g + 8 * r] = l[r];
+      }
+      if (warp > 0 && g + 8 * r < q_rows) {
+        float* dst = s_out + ((warp - 1) * 16 + g + 8 * r) * PITCH + 2 * t4;
+#pragma unroll
+        for (int d = 0; d < HD / 8; ++d) *reinterpret_cast<float2*>(dst + 8 * d) = make_float2(o[d][2 * r], o[d][2 * r + 1]);
+      }
+    }
+    consumers_sync();
+    const bool whole = todo == item.s.chunks;
+    const int first_cta = whole ? c : (int)(((item.item_begin + 1) * G - 1) / T);
+    if (warp == 0) {
+      float* part = p.parts + ((size_t)c * 2 + (c == first_cta ? 1 : 0)) * 16 * PITCH;   // an item that begins here and goes on: slot 1
+#pragma unroll
+      for (int r = 0; r < (WIDE ? 2 : 1); ++r) {
+        const int row = g + 8 * r;
+        if (row >= q_rows) continue;
+        float M = -INFINITY, L = 0.f, f[TK_WARPS];
+#pragma unroll
+        for (int w = 0; w < TK_WARPS; ++w) M = fmaxf(M, s_stat[w * 16 + row]);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < TK_WARPS; ++w) {
+          f[w] = fast_exp2(s_stat[w * 16 + row] - ref);
+          L = fmaf(f[w], s_stat[TK_WARPS * 16 + w * 16 + row], L);
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const long long out_row = (long long)item.row;
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + out_row * p.a.out_stride + (head0 + row) * HD + 2 * t4;
+#pragma unroll
+        for (int d = 0; d < HD / 8; ++d) {
+          float2 v = make_float2(o[d][2 * r] * f[0], o[d][2 * r + 1] * f[0]);
+#pragma unroll
+          for (int w = 1; w < TK_WARPS; ++w) {
+            const float2 x = *reinterpret_cast<const float2*>(s_out + ((w - 1) * 16 + row) * PITCH + 8 * d + 2 * t4);
+            v.x = fmaf(f[w], x.x, v.x); v.y = fmaf(f[w], x.y, v.y);
+          }
+          if (whole) *reinterpret_cast<uint32_t*>(out + 8 * d) = pack_bf16(v.x * inv, v.y * inv);
+          else *reinterpret_cast<float2*>(part + row * PITCH + 8 * d + 2 * t4) = v;
+        }
+        if (t4 == 0) {
+          if (!whole) { part[row * PITCH + HD] = M; part[row * PITCH + HD + 1] = L; }
+          else if (p.a.lse) p.a.lse[out_row * p.a.heads + head0 + row] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+        }
+      }
+    }
+    if (!whole) {
+      // ---- the last of the item's CTAs joins their parts in order
+      const int last_cta = (int)(((item.item_begin + item.s.chunks) * G - 1) / T);
+      if (warp == 0) {
+        __syncwarp();
+        int is_last = 0;
+        if (lane == 0) {
+          __threadfence();
+          is_last = chain_arrive_count(p.arrived + first_cta) == last_cta - first_cta;
+          s_first[1] = is_last;
+        }
+      }
+      consumers_sync();
+      if (s_first[1]) {
+        for (int e = threadIdx.x; e < q_rows * (HD / 4); e += TK_WARPS * 32) {
+          const int row = e / (HD / 4), d = (e - row * (HD / 4)) * 4;
+          const size_t step = (size_t)2 * 16 * PITCH;
+          const float* at0 = p.parts + ((size_t)first_cta * 2 + 1) * 16 * PITCH + row * PITCH;   // the first CTA's slot 1, the others' slot 0
+          const float* at = p.parts + (size_t)(first_cta + 1) * step + row * PITCH;
+          const int others = last_cta - first_cta;
+          float M = __ldcg(at0 + HD);
+#pragma unroll 8
+          for (int k = 0; k < others; ++k) M = fmaxf(M, __ldcg(at + k * step + HD));
+          const float ref = M == -INFINITY ? 0.f : M;
+          float f = fast_exp2(__ldcg(at0 + HD) - ref);
+          float L = f * __ldcg(at0 + HD + 1);
+          float4 v = __ldcg(reinterpret_cast<const float4*>(at0 + d));
+          v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+#pragma unroll 8
+          for (int k = 0; k < others; ++k) {
+            const float2 st = __ldcg(reinterpret_cast<const float2*>(at + k * step + HD));
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(at + k * step + d));
+            f = fast_exp2(st.x - ref);
+            L = fmaf(f, st.y, L);
+            v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+          }
+          const float inv = L == 0.f ? 0.f : 1.f / L;
+          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + (long long)item.row * p.a.out_stride + (head0 + row) * HD + d;
+          *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
+          if (d == 0 && p.a.lse) p.a.lse[(long long)item.row * p.a.heads + head0 + row] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+        }
+        if (threadIdx.x == 0) p.arrived[first_cta] = 0;
+      }
+    }
+    if (n < n_units) {
+      cur.chunk += todo - 1;
+      next_unit(p, items, cur);
+    }
+  }
+}
+
+}  // namespace
+
+size_t pages_token_part_bytes(const PageView& pv, int grid) {
+  return ((size_t)grid * 2 * 16 * (pv.hd + 4) * 4 + 255) / 256 * 256 + ((size_t)grid * 4 + 255) / 256 * 256;
+}
+
+template <typename F> static cudaError_t for_token_kernels(int hd, F f) {
+  cudaError_t e = cudaSuccess;
+  if (hd == 64) { e = f(pages_token_kernel<64, false>, token_smem<64>()); return e ? e : f(pages_token_kernel<64, true>, token_smem<64>()); }
+  e = f(pages_token_kernel<128, false>, token_smem<128>());
+  return e ? e : f(pages_token_kernel<128, true>, token_smem<128>());
+}
+
+cudaError_t pages_token_prepare(int hd) {
+  return for_token_kernels(hd, [](auto k, size_t smem) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+}
+
+// parts: pages_token_part_bytes, its counters zero.  grid: the SMs.
+cudaError_t launch_pages_token(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int grid, cudaStream_t st) {
+  TokenParams p;
+  p.pv = pv; p.rows = rows; p.a = a;
+  p.group = a.heads / pv.H; p.tiles = (p.group + 15) / 16;
+  p.parts = (float*)parts;
+  p.arrived = (int32_t*)((char*)parts + ((size_t)grid * 2 * 16 * (pv.hd + 4) * 4 + 255) / 256 * 256);
+  auto go = [&](auto k, size_t smem) { launch_pdl(k, grid, TK_THREADS, smem, st, *(const CUtensorMap*)map, p); };
+  const bool wide = p.group > 8;
+  if (pv.hd == 64) wide ? go(pages_token_kernel<64, true>, token_smem<64>()) : go(pages_token_kernel<64, false>, token_smem<64>());
+  else wide ? go(pages_token_kernel<128, true>, token_smem<128>()) : go(pages_token_kernel<128, false>, token_smem<128>());
+  return cudaGetLastError();
+}
+
+}  // namespace rd

@@ -83,6 +83,7 @@ cudaError_t launch_gemm_simt(int dtype, int epi, const SimtOperands& p, const Si
 // Tensor-core (tcgen05) projection, bf16 only.  Operands are passed as TMA descriptors.
 int tc_make_map(void* out_map, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_rows);
 int tc_make_map_halves(void* out_map, const void* ptr, uint64_t rows, uint32_t box_rows);
+int tc_make_map_parts(void* out_map, const void* ptr, uint64_t rows, uint32_t cols, uint32_t box_rows);
 int tc_weight_box_rows();
 int tc_pick_mt(int m_max);
 size_t tc_partial_floats(int grid, int mt);
