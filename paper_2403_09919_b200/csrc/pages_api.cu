@@ -21,6 +21,7 @@ constexpr int TOKEN_MAX_GRID = 160;   // upper bound of the SM count that the pa
 
 struct rd_pages {
   MapBox map_parts;   // the pool's rows, min(page_size, 64) to a box (bf16)
+  MapBox map_rows;    // the same in boxes of 64 columns
   PageView pv;
   int dtype, device;
   int32_t* scratch;
@@ -153,12 +154,15 @@ int redrafter_pages_init(const rd_page_cache* cache, void* workspace, size_t ws_
   if (e == cudaSuccess && pv.es == 2) {
     if (h->grid > TOKEN_MAX_GRID) h->grid = TOKEN_MAX_GRID;
     const uint64_t pool_rows = (uint64_t)pv.n_layers * 2 * pv.n_pages * pv.H * pv.ps;
-    const int rc = tc_make_map_parts(h->map_parts.bytes, pv.pool, pool_rows, pv.hd, pv.ps < 64 ? pv.ps : 64);
+    const uint32_t box = pv.ps < 64 ? pv.ps : 64;
+    int rc = tc_make_map_parts(h->map_parts.bytes, pv.pool, pool_rows, pv.hd, box);
+    if (!rc) rc = tc_make_map(h->map_rows.bytes, pv.pool, pool_rows, pv.hd, box);
     if (rc) {
       delete h;
       return init_fail(RD_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d for the pool", rc);
     }
     e = pages_token_prepare(pv.hd);
+    if (e == cudaSuccess) e = pages_rows_prepare(pv.hd);
     if (e == cudaSuccess) e = cudaMemsetAsync(h->parts, 0, pages_token_part_bytes(pv, TOKEN_MAX_GRID), 0);
   }
   if (e == cudaSuccess) e = cudaMemsetAsync(workspace, 0, 256, 0);
@@ -273,6 +277,7 @@ int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, c
   a.window = window; a.sinks = window ? sinks : 0;
   a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)h->pv.hd);
   if (h->pv.es == 2 && rows.max_rows == 1) PCK(launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, (cudaStream_t)stream));
+  else if (h->pv.es == 2) PCK(launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, (cudaStream_t)stream));
   else PCK(launch_pages_attention_plain(h->pv, h->dtype, rows, a, (cudaStream_t)stream));
   h->launches++;
   return RD_OK;
