@@ -75,7 +75,7 @@ cudaError_t pages_token_prepare(int hd);
 cudaError_t launch_pages_token(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int grid, cudaStream_t st);
 // many rows per sequence, bf16
 cudaError_t pages_rows_prepare(int hd);
-cudaError_t launch_pages_rows(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, cudaStream_t st);
+cudaError_t launch_pages_rows(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, int sms, cudaStream_t st);
 cudaError_t launch_pages_attention_plain(const PageView& pv, int dtype, const PageRows& rows, const PageAttention& a, cudaStream_t st);
 
 }  // namespace rd

@@ -277,7 +277,7 @@ int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, c
   a.window = window; a.sinks = window ? sinks : 0;
   a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)h->pv.hd);
   if (h->pv.es == 2 && rows.max_rows == 1) PCK(launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, (cudaStream_t)stream));
-  else if (h->pv.es == 2) PCK(launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, (cudaStream_t)stream));
+  else if (h->pv.es == 2) PCK(launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, h->grid, (cudaStream_t)stream));
   else PCK(launch_pages_attention_plain(h->pv, h->dtype, rows, a, (cudaStream_t)stream));
   h->launches++;
   return RD_OK;
