@@ -17,8 +17,8 @@
 // The CTAs stay (one per SM) and take one item after another, so that the next one's Q, K and V are on their way while the last
 // products and the output of one are finished.
 // Roles: warp 0 finds the items and loads K and V by TMA, warp 1 MMA (the whole warp runs the loop, an elected lane issues), warps
-// 2 and 3 look through V, warps 4-7 softmax A, 8-11 softmax B.  Registers: 384 x 168 = 64,512 at launch; 4 warps go down to 96 and 8 up to 200
-// (128 x 96 + 256 x 200 = 63,488).  Every wait is bounded; on expiry the CTA reports and leaves.
+// 2 and 3 look through V, warps 4-7 softmax A, 8-11 softmax B.  Registers: 384 x 168 = 64,512 at launch; 4 warps go down to 72 and 8 up to 216
+// (128 x 72 + 256 x 216 = 64,512).  Every wait is bounded; on expiry the CTA reports and leaves.
 //
 // Anything may lie in keys that a row does not see.  Scores are masked by selection.  V's rows that no row of the CTA sees are
 // overwritten by zeros, and chunks that only some rows see are looked through: where such a chunk holds NaN or infinities,
@@ -41,6 +41,7 @@ constexpr int RW_STAGES = 2;
 constexpr int RW_THREADS = 384;
 constexpr uint32_t RW_BLOCK = 128 * 128;   // bytes of 128 rows of 64 columns
 constexpr float RW_SLACK = 8.f;
+constexpr int RW_SLOTS = 4;                // published items
 
 struct RowsParams {
   PageView pv;
@@ -54,62 +55,66 @@ __device__ __forceinline__ uint64_t desc_mnmajor_v(uint32_t addr) {
 __device__ __forceinline__ void tmem_st32_u32(uint32_t taddr, const uint32_t (&r)[32]) {
   tmem_st32(taddr, reinterpret_cast<const float*>(r));
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&u)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+        "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(taddr));
+}
 // Bits 0 .. n-1.
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
-// What the rows of a CTA see, as a list of boxes.
-struct BoxList {
-  int box_log2, sink_boxes, first_box, n_boxes;
-  int sinks, start, end;   // keys that some row sees: [0, sinks) and [start, end)
-  __device__ __forceinline__ int base(int b) const {   // first key of box b; behind the list: out of sight of everything
-    return b >= n_boxes ? 0x7fffff00 : (b < sink_boxes ? b : first_box + b - sink_boxes) << box_log2;
-  }
-  __device__ __forceinline__ bool seen_by_all(int b, int pos_first, int pos_last, int window) const {   // rows at these positions
-    const int k0 = base(b), k1 = k0 + (1 << box_log2) - 1;
-    return k1 <= pos_first && (window == 0 || k0 > pos_last - window || k1 < sinks);
-  }
-};
-
-// What a CTA works on next, published by the producer warp in two slots.
+// What a CTA works on next, worked out by the producer warp and published two items ahead.
 struct RowsItem {
   int head, row0, n_rows, pos0, seq;   // head -1: there is nothing left; pos0: position of the first row
-  int unclean;                         // V holds NaN or infinities that only some of the rows see
-};
+  // The keys as a list of boxes: 0 .. sink_boxes - 1 hold sinks, those from `first` on are box b + skew of the sequence, and the
+  // places between them are left empty.
+  int n_chunks, sink_boxes, skew, first;
+  int start, end, sinks;      // keys that some row sees: [0, sinks) and [start, end)
+  int to_a, from_b, to_b;     // chunks that a tile works on; A from the first
+  int all_from, all_to_a, all_to_b, all_from_b;   // chunks that every row of a tile (A: all_from .. all_to_a) sees whole
+  int unclean;                // V holds NaN or infinities that only some of the rows see
 
-// ... and what follows from it for the keys.
-struct RowsPlan {
-  BoxList bl;
-  int n_tiles, n_chunks, per_chunk;
-  int to_a, from_b, to_b;   // chunks that a tile works on; A from the first
   __device__ __forceinline__ int from(int tile) const { return tile ? from_b : 0; }
   __device__ __forceinline__ int to(int tile) const { return tile ? to_b : to_a; }
   __device__ __forceinline__ bool active(int tile, int c) const { return c >= from(tile) && c < to(tile); }
   __device__ __forceinline__ bool has(int tile) const { return to(tile) > from(tile); }
+  // first key of box b; a place that is left empty: out of sight of everything
+  __device__ __forceinline__ int base(int b, int box_log2) const {
+    return b < sink_boxes ? b << box_log2 : b < first ? 0x7fffff00 : (b + skew) << box_log2;
+  }
 };
 
-__device__ __forceinline__ RowsPlan plan_rows(const RowsItem& it, int window, int sinks, int box_log2) {
-  RowsPlan r;
-  BoxList& bl = r.bl;
-  const int box = 1 << box_log2;
-  bl.box_log2 = box_log2;
-  r.n_tiles = it.n_rows > RW_TILE ? 2 : 1;
-  bl.end = max(0, it.pos0 + it.n_rows);
-  bl.start = window > 0 ? max(0, it.pos0 - window + 1) : 0;
-  bl.sinks = min(sinks, bl.start);
-  bl.first_box = bl.start >> box_log2;
-  bl.sink_boxes = min((bl.sinks + box - 1) >> box_log2, bl.first_box);
-  auto boxes_to = [&](int end) { return end > 0 ? bl.sink_boxes + ((end + box - 1) >> box_log2) - bl.first_box : 0; };
-  bl.n_boxes = boxes_to(bl.end);
-  r.per_chunk = RW_KEYS >> box_log2;
-  const int pc_log2 = 7 - box_log2;
-  r.n_chunks = (bl.n_boxes + r.per_chunk - 1) >> pc_log2;
+__device__ __forceinline__ void plan_rows(RowsItem& r, int window, int sinks, int box_log2) {
+  const int box = 1 << box_log2, pc_log2 = 7 - box_log2, per_chunk = 1 << pc_log2;
+  const bool two = r.n_rows > RW_TILE;
+  r.end = max(0, r.pos0 + r.n_rows);
+  r.start = window > 0 ? max(0, r.pos0 - window + 1) : 0;
+  r.sinks = min(sinks, r.start);
+  const int first_box = r.start >> box_log2, end_box = (r.end + box - 1) >> box_log2;
+  r.sink_boxes = min((r.sinks + box - 1) >> box_log2, first_box);
+  r.n_chunks = r.end > 0 ? (r.sink_boxes + end_box - first_box + per_chunk - 1) >> pc_log2 : 0;
+  // The list ends with a chunk: what is left empty lies before the window's boxes, so that the diagonal of rows that end on a
+  // multiple of 128 crosses one chunk a tile.
+  r.skew = end_box - (r.n_chunks << pc_log2);
+  r.first = first_box - r.skew;
   // A stops behind its own last row's key, B begins (without sinks) where its first row's window does
-  const int boxes_a = r.n_tiles == 2 ? boxes_to(max(0, min(it.pos0 + RW_TILE, bl.end))) : bl.n_boxes;
-  const int start_b = window > 0 ? max(0, it.pos0 + RW_TILE - window + 1) : 0;
-  r.to_a = min(r.n_chunks, (boxes_a + r.per_chunk - 1) >> pc_log2);
-  r.from_b = r.n_tiles == 2 && sinks == 0 ? max(0, (start_b >> box_log2) - bl.first_box) >> pc_log2 : 0;
-  r.to_b = r.n_tiles == 2 ? r.n_chunks : 0;
-  return r;
+  const int end_a = max(0, min(r.pos0 + RW_TILE, r.end)), start_b = window > 0 ? max(0, r.pos0 + RW_TILE - window + 1) : 0;
+  r.to_a = !two ? r.n_chunks : end_a > 0 ? min(r.n_chunks, (((end_a + box - 1) >> box_log2) - r.skew + per_chunk - 1) >> pc_log2) : 0;
+  r.from_b = two && sinks == 0 && r.n_chunks > 0 ? max(0, (start_b >> box_log2) - r.skew) >> pc_log2 : 0;
+  r.to_b = two ? r.n_chunks : 0;
+  // Chunk c of the window's part holds the keys k0 .. k0 + 127, k0 = (c * per_chunk + skew) * box.  Rows at positions p .. q see
+  // all of it if k0 + 127 <= p and k0 > q - window.
+  auto all_to = [&](int p) { return p < RW_KEYS - 1 ? 0 : (((p - (RW_KEYS - 1)) >> box_log2) - r.skew + per_chunk) >> pc_log2; };
+  auto all_from = [&](int q) {
+    const int c0 = (r.first + per_chunk - 1) >> pc_log2;   // the first chunk without sinks and empty places
+    return window > 0 && q >= window ? max(c0, (((q - window + box) >> box_log2) - r.skew + per_chunk - 1) >> pc_log2) : c0;
+  };
+  r.all_from = all_from(r.pos0 + min(r.n_rows, RW_TILE) - 1);
+  r.all_to_a = all_to(r.pos0);
+  r.all_from_b = all_from(r.pos0 + r.n_rows - 1);
+  r.all_to_b = all_to(r.pos0 + RW_TILE);
 }
 
 __device__ __forceinline__ uint64_t pair(float a, float b) {
@@ -137,7 +142,8 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool t
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16u : 0u) : "memory");
 }
 
-template <int HD> constexpr size_t rows_smem() { return 1024 + (size_t)(2 + 2 * RW_STAGES) * (HD / 64) * RW_BLOCK + 512; }
+constexpr int RW_STAGE_OUT = 32 * 128;     // bytes of a softmax warp's output on its way: 32 rows of 64 columns
+template <int HD> constexpr size_t rows_smem() { return 1024 + (size_t)(2 + 2 * RW_STAGES) * (HD / 64) * RW_BLOCK + 8 * RW_STAGE_OUT + 1024; }
 
 template <int HD>
 __global__ void __launch_bounds__(RW_THREADS, 1)
@@ -148,14 +154,14 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
-  const uint32_t sQ = base, sK = sQ + 2 * TILE, sV = sK + RW_STAGES * TILE, bar0 = sV + RW_STAGES * TILE;
+  const uint32_t sQ = base, sK = sQ + 2 * TILE, sV = sK + RW_STAGES * TILE, sO = sV + RW_STAGES * TILE, bar0 = sO + 8 * RW_STAGE_OUT;
   enum { K_FULL = 0, K_EMPTY = 2, V_FULL = 4, V_OK = 6, V_EMPTY = 8, Q_FULL = 10, S_FULL = 12, P_HALF = 14, P_FULL = 16, O_FULL = 18, O_EMPTY = 20,
-         ITEM_FULL = 22, ITEM_EMPTY = 24, N_BARS = 26 };
+         ITEM_FULL = 22, ITEM_EMPTY = 26, N_BARS = 30 };
   auto bar = [&](int i) { return bar0 + 8u * i; };
   uint8_t* misc = gen + (bar0 - base) + 8 * N_BARS;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);
-  volatile RowsItem* s_item = reinterpret_cast<volatile RowsItem*>(misc + 16);   // [2]
+  RowsItem* s_item = reinterpret_cast<RowsItem*>(misc + 16);   // [RW_SLOTS]; guarded by ITEM_FULL and ITEM_EMPTY
   const PageView& pv = p.pv;
 
   if (warp == 1) {
@@ -169,8 +175,8 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
       mbar_init(bar(V_FULL + s), 1); mbar_init(bar(V_OK + s), 2); mbar_init(bar(V_EMPTY + s), 1);
       mbar_init(bar(Q_FULL + s), 4); mbar_init(bar(S_FULL + s), 1); mbar_init(bar(P_HALF + s), 4); mbar_init(bar(P_FULL + s), 4);
       mbar_init(bar(O_FULL + s), 1); mbar_init(bar(O_EMPTY + s), 4);
-      mbar_init(bar(ITEM_FULL + s), 1); mbar_init(bar(ITEM_EMPTY + s), 1 + 2 + 8);
     }
+    for (int s = 0; s < RW_SLOTS; ++s) { mbar_init(bar(ITEM_FULL + s), 1); mbar_init(bar(ITEM_EMPTY + s), 1 + 2 + 8); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -180,94 +186,96 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
   const uint32_t tmem = *tmem_slot;
   pdl_enter();
 
-  const int window = p.a.window, sinks = p.a.sinks, group = p.a.heads / pv.H, box_log2 = min(pv.ps_log2, 6);
+  const int window = p.a.window, sinks = p.a.sinks, group = p.a.heads / pv.H, box_log2 = min(pv.ps_log2, 6), per_chunk = RW_KEYS >> box_log2;
   auto wait_warp = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag, pv.status)) != 0; };
-  // item k of this CTA, for the warps that are told: false when a wait gave up
-  auto next_item = [&](int k, RowsItem& it) {
-    if (!wait_warp(bar(ITEM_FULL + (k & 1)), (uint32_t)((k >> 1) & 1))) return false;
-    volatile RowsItem& s = s_item[k & 1];
-    it.head = s.head; it.row0 = s.row0; it.n_rows = s.n_rows; it.pos0 = s.pos0; it.seq = s.seq;
-    return true;
-  };
+  // item k of this CTA is in its slot, for the warps that are told: false when the wait gave up
+  auto next_item = [&](int k) { return wait_warp(bar(ITEM_FULL + (k & 3)), (uint32_t)((k >> 2) & 1)); };
   auto release_item = [&](int k) {
     __syncwarp();
-    if (lane == 0) mbar_arrive(bar(ITEM_EMPTY + (k & 1)));
+    if (lane == 0) mbar_arrive(bar(ITEM_EMPTY + (k & 3)));
   };
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 0) {
       // ===================== producer: what comes next, and K and V by TMA (lane = (box, half) of the chunk) =====================
       const int n = p.rows.n;
-      auto pairs_of = [&](int i) {
-        if (i >= n) return 0;
-        int first, m;
-        page_rows_of(p.rows, i, &first, &m);
-        return m > p.rows.max_rows ? 0 : (m + 2 * RW_TILE - 1) / (2 * RW_TILE);
+      // this lane's entry of a group of 32: its first row, rows, pairs of tiles, sequence and length
+      int e_first = 0, e_m = 0, e_pairs = 0, e_seq = -1, e_len = 0, e_group = -1;
+      auto look_up = [&](int i0) {
+        if (i0 == e_group) return;
+        e_group = i0; e_first = e_m = e_pairs = e_len = 0; e_seq = -1;
+        const int i = i0 + lane;
+        if (i >= n) return;
+        e_seq = page_seq_of(pv, p.rows.seqs, i);
+        page_rows_of(p.rows, i, &e_first, &e_m);
+        if (e_seq >= 0) e_len = page_len_of(pv, e_seq);
+        e_pairs = e_m > p.rows.max_rows ? 0 : (e_m + 2 * RW_TILE - 1) / (2 * RW_TILE);
       };
       int total = 0;   // pairs of tiles of all entries
-      for (int i0 = 0; i0 < n; i0 += 32) total += __reduce_add_sync(0xffffffffu, pairs_of(i0 + lane));
-      if (blockIdx.x == 0)   // entries that cannot be answered
-        for (int i = lane; i < n; i += 32) {
-          int first, m;
-          page_rows_of(p.rows, i, &first, &m);
-          if (m > p.rows.max_rows || (m > 0 && page_seq_of(pv, p.rows.seqs, i) < 0)) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
-        }
+      for (int i0 = 0; i0 < n; i0 += 32) {
+        look_up(i0);
+        total += __reduce_add_sync(0xffffffffu, e_pairs);
+        if (blockIdx.x == 0 && (e_m > p.rows.max_rows || (e_m > 0 && e_seq < 0))) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);   // cannot be answered
+      }
       const long long pool_rows = (long long)pv.n_layers * 2 * pv.n_pages * pv.H * pv.ps, plane_rows = (long long)pv.n_pages * pv.H * pv.ps;
       const int box = lane / HALVES, half = lane - box * HALVES;
       const uint32_t place = (uint32_t)(half * RW_BLOCK + ((box << box_log2) * 128));
       bool ok = true;
       uint32_t g = 0;   // chunks of K and V so far
-      for (int k = 0; ok; ++k) {
-        // the pairs are handed out last first: later rows of a sequence have more keys
+      // works out item k of this CTA and publishes it; the pairs are handed out last first: later rows of a sequence have more keys
+      auto publish = [&](int k) {
         const long long index = blockIdx.x + (long long)k * gridDim.x;
         const int slot = index < (long long)total * p.a.heads ? total - 1 - (int)(index / p.a.heads) : -1;
-        RowsItem it{-1, 0, 0, 0, -1, 0};
+        RowsItem it{};
+        it.head = -1;
         if (slot >= 0) {
-          int before = 0, entry = 0, tile_pair = 0;
+          int before = 0;
           for (int i0 = 0; i0 < n; i0 += 32) {
-            const int mine = pairs_of(i0 + lane);
-            int incl = mine;
+            look_up(i0);
+            int incl = e_pairs;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
               const int v = __shfl_up_sync(0xffffffffu, incl, o);
               if (lane >= o) incl += v;
             }
-            const uint32_t here = __ballot_sync(0xffffffffu, slot >= before + incl - mine && slot < before + incl);
+            const int at = before + incl - e_pairs;
+            const uint32_t here = __ballot_sync(0xffffffffu, slot >= at && slot < at + e_pairs);
             if (here) {
               const int src = __ffs(here) - 1;
-              entry = i0 + src;
-              tile_pair = slot - before - __shfl_sync(0xffffffffu, incl - mine, src);
+              const int skip = (slot - __shfl_sync(0xffffffffu, at, src)) * 2 * RW_TILE, m = __shfl_sync(0xffffffffu, e_m, src);
+              it.head = (int)(index % p.a.heads);
+              it.row0 = __shfl_sync(0xffffffffu, e_first, src) + skip;
+              it.n_rows = min(2 * RW_TILE, m - skip);
+              it.pos0 = __shfl_sync(0xffffffffu, e_len, src) - m + skip;
+              it.seq = __shfl_sync(0xffffffffu, e_seq, src);
+              plan_rows(it, window, sinks, box_log2);
               break;
             }
             before += __shfl_sync(0xffffffffu, incl, 31);
           }
-          int first, m;
-          page_rows_of(p.rows, entry, &first, &m);
-          it.seq = page_seq_of(pv, p.rows.seqs, entry);
-          const int len = it.seq >= 0 ? page_len_of(pv, it.seq) : 0, skip = tile_pair * 2 * RW_TILE;
-          it.head = (int)(index % p.a.heads);
-          it.row0 = first + skip;
-          it.n_rows = min(2 * RW_TILE, m - skip);
-          it.pos0 = len - m + skip;
         }
-        if (k >= 2 && !(ok = wait_warp(bar(ITEM_EMPTY + (k & 1)), (uint32_t)(((k >> 1) & 1) ^ 1)))) break;
+        if (k >= RW_SLOTS && !(ok = wait_warp(bar(ITEM_EMPTY + (k & 3)), (uint32_t)(((k >> 2) & 1) ^ 1)))) return;
         if (lane == 0) {
-          volatile RowsItem& s = s_item[k & 1];
-          s.head = it.head; s.row0 = it.row0; s.n_rows = it.n_rows; s.pos0 = it.pos0; s.seq = it.seq; s.unclean = 0;
-          mbar_arrive(bar(ITEM_FULL + (k & 1)));
+          s_item[k & 3] = it;
+          mbar_arrive(bar(ITEM_FULL + (k & 3)));
         }
         __syncwarp();
-        if (it.head < 0) break;
-        const RowsPlan r = plan_rows(it, window, sinks, box_log2);
+      };
+      publish(0);
+      for (int k = 0; ok; ++k) {
+        if (s_item[k & 3].head < 0) break;
+        publish(k + 1);
+        if (!ok) break;
+        const RowsItem it = s_item[k & 3];
         const int kv_head = it.head / group;
-        const bool mine = box < r.per_chunk;
+        const bool mine = box < per_chunk;
         auto row_of = [&](int c, int which) -> int {   // row of the pool at which this lane's box begins
-          const int key = r.bl.base(c * r.per_chunk + box);
-          if (!mine || key >= r.bl.end) return (int)pool_rows;   // (behind the pool's last row the copy fills in zeros)
+          const int key = it.base(c * per_chunk + box, box_log2);
+          if (!mine || key >= it.end) return (int)pool_rows;   // (behind the pool's last row the copy fills in zeros)
           const int page = pv.table[(size_t)it.seq * pv.max_pages + (key >> pv.ps_log2)];
           if ((unsigned)page >= (unsigned)pv.n_pages) {   // trimmed, or bad: reported where a row sees something of it
-            if (key + (1 << box_log2) > r.bl.start || key < r.bl.sinks) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
+            if (key + (1 << box_log2) > it.start || key < it.sinks) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
             return (int)pool_rows;
           }
           return (int)((((long long)p.a.layer * 2 * pv.n_pages + page) * pv.H + kv_head) * pv.ps + (key & (pv.ps - 1)) + which * plane_rows);
@@ -282,16 +290,16 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
           if (x >= 2 && !(ok = wait_warp(bar(K_EMPTY + s), ((x >> 1) & 1) ^ 1u))) return;
           load(sK + s * TILE, bar(K_FULL + s), row);
         };
-        if (r.n_chunks > 0) load_k(0, row_of(0, 0));
-        for (int c = 0; c < r.n_chunks && ok; ++c) {   // K a chunk ahead of V: its slot comes free earlier
+        if (it.n_chunks > 0) load_k(0, row_of(0, 0));
+        for (int c = 0; c < it.n_chunks && ok; ++c) {   // K a chunk ahead of V: its slot comes free earlier
           const uint32_t x = g + c, s = x & 1;
-          const int vrow = row_of(c, 1), krow = c + 1 < r.n_chunks ? row_of(c + 1, 0) : 0;
-          if (c + 1 < r.n_chunks) load_k(c + 1, krow);
+          const int vrow = row_of(c, 1), krow = c + 1 < it.n_chunks ? row_of(c + 1, 0) : 0;
+          if (c + 1 < it.n_chunks) load_k(c + 1, krow);
           if (!ok) break;
           if (x >= 2 && !(ok = wait_warp(bar(V_EMPTY + s), ((x >> 1) & 1) ^ 1u))) break;
           load(sV + s * TILE, bar(V_FULL + s), vrow);
         }
-        g += r.n_chunks;
+        g += it.n_chunks;
       }
       if (!ok || *abort_flag) {   // copies already issued land before the CTA's shared memory is given back
         const unsigned long long t0 = now_ns();
@@ -306,14 +314,11 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
       uint32_t g = 0, np_a = 0, np_b = 0, ni_a = 0, ni_b = 0;   // chunks; chunks and items that a tile has worked on
       bool ok = true;
       for (int k = 0; ok; ++k) {
-        RowsItem it;
-        if (!next_item(k, it) || it.head < 0) break;
-        const RowsPlan r = plan_rows(it, window, sinks, box_log2);
+        if (!next_item(k) || s_item[k & 3].head < 0) break;
+        const RowsItem it = s_item[k & 3];
         auto issue_qk = [&](int tile, int c) {
-          if (c == r.from(tile)) {   // the tile's first: its Q, and its output read
-            const uint32_t ni = tile ? ni_b : ni_a;
-            if (!wait_warp(bar(Q_FULL + tile), ni & 1)) return false;
-            if (ni > 0 && !wait_warp(bar(O_EMPTY + tile), (ni - 1) & 1)) return false;
+          if (c == it.from(tile)) {   // the tile's first of this item
+            if (!wait_warp(bar(Q_FULL + tile), (tile ? ni_b : ni_a) & 1)) return false;
             tc_fence_after();
           }
           const uint64_t qd = desc_kmajor(sQ + (uint32_t)tile * TILE), kd = desc_kmajor(sK + ((g + c) & 1) * TILE);
@@ -328,23 +333,25 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
           __syncwarp();
           return true;
         };
-        if (r.n_chunks > 0) {
+        if (it.n_chunks > 0) {
           if (!(ok = wait_warp(bar(K_FULL + (g & 1)), (g >> 1) & 1))) break;
           tc_fence_after();
           for (int tile = 0; tile < 2 && ok; ++tile)
-            if (r.active(tile, 0)) ok = issue_qk(tile, 0);
+            if (it.active(tile, 0)) ok = issue_qk(tile, 0);
           if (!ok) break;
           if (leader) umma_commit(bar(K_EMPTY + (g & 1)));
           __syncwarp();
         }
-        for (int c = 0; c < r.n_chunks && ok; ++c) {
+        for (int c = 0; c < it.n_chunks && ok; ++c) {
           const uint32_t x = g + c, s = x & 1;
           if (!(ok = wait_warp(bar(V_OK + s), (x >> 1) & 1))) break;
-          if (c + 1 < r.n_chunks && !(ok = wait_warp(bar(K_FULL + (s ^ 1)), ((x + 1) >> 1) & 1))) break;
+          if (c + 1 < it.n_chunks && !(ok = wait_warp(bar(K_FULL + (s ^ 1)), ((x + 1) >> 1) & 1))) break;
 #pragma unroll
           for (int tile = 0; tile < 2; ++tile) {
-            if (r.active(tile, c)) {
+            if (it.active(tile, c)) {
               const uint64_t vd = desc_mnmajor_v(sV + s * TILE);
+              const uint32_t ni = tile ? ni_b : ni_a;
+              if (c == it.from(tile) && ni > 0 && !(ok = wait_warp(bar(O_EMPTY + tile), (ni - 1) & 1))) break;   // the output before has been read
               for (int hf = 0; hf < 2; ++hf) {   // the weights come in two halves
                 if (!(ok = wait_warp(bar((hf ? P_FULL : P_HALF) + tile), (tile ? np_b : np_a) & 1))) break;
                 tc_fence_after();
@@ -352,25 +359,25 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
 #pragma unroll
                   for (int kk = 0; kk < RW_KEYS / 32; ++kk)
                     umma_bf16_ts(tmem + 256u + (uint32_t)tile * 128u, tmem + (uint32_t)tile * 128u + (uint32_t)(hf * 4 + kk) * 8u,
-                                 vd + (uint64_t)((hf * 4 + kk) * 128), idesc_pv, (c > r.from(tile) || hf > 0 || kk > 0) ? 1u : 0u);
-                  if (hf && c + 1 == r.to(tile)) umma_commit(bar(O_FULL + tile));
+                                 vd + (uint64_t)((hf * 4 + kk) * 128), idesc_pv, (c > it.from(tile) || hf > 0 || kk > 0) ? 1u : 0u);
+                  if (hf && c + 1 == it.to(tile)) umma_commit(bar(O_FULL + tile));
                 }
                 __syncwarp();
               }
               if (!ok) break;
               ++(tile ? np_b : np_a);
-              if (c + 1 == r.to(tile)) ++(tile ? ni_b : ni_a);
+              if (c + 1 == it.to(tile)) ++(tile ? ni_b : ni_a);
             }
-            if (c + 1 < r.n_chunks && r.active(tile, c + 1) && !(ok = issue_qk(tile, c + 1))) break;
+            if (c + 1 < it.n_chunks && it.active(tile, c + 1) && !(ok = issue_qk(tile, c + 1))) break;
           }
           if (!ok) break;
           if (leader) {
             umma_commit(bar(V_EMPTY + s));
-            if (c + 1 < r.n_chunks) umma_commit(bar(K_EMPTY + (s ^ 1)));
+            if (c + 1 < it.n_chunks) umma_commit(bar(K_EMPTY + (s ^ 1)));
           }
           __syncwarp();
         }
-        g += r.n_chunks;
+        g += it.n_chunks;
         release_item(k);
       }
     } else {
@@ -379,55 +386,53 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
       uint32_t g = 0;
       bool ok = true;
       for (int k = 0; ok; ++k) {
-        RowsItem it;
-        if (!next_item(k, it) || it.head < 0) break;
-        const RowsPlan r = plan_rows(it, window, sinks, box_log2);
-        const int pos_last = it.pos0 + it.n_rows - 1;
-        for (int c = 0; c < r.n_chunks; ++c) {
+        if (!next_item(k) || s_item[k & 3].head < 0) break;
+        const RowsItem it = s_item[k & 3];
+        for (int c = 0; c < it.n_chunks; ++c) {
           const uint32_t x = g + c, s = x & 1;
-          bool all = true;   // every row of the CTA sees all of the chunk
-          for (int b = 0; b < r.per_chunk; ++b) all = all && r.bl.seen_by_all(c * r.per_chunk + b, it.pos0, pos_last, window);
+          const bool all = c >= it.all_from_b && c < it.all_to_a;   // every row of the CTA sees all of the chunk
           if (!(ok = wait_warp(bar(V_FULL + s), (x >> 1) & 1))) break;
           if (!all) {
-            bool unclean = false;
+            uint32_t bad = 0;   // bits 15 and 31: an exponent of all ones among what was looked at
             uint8_t* at0 = gen + (sV - base) + s * TILE + t * 16;
-#pragma unroll 1
+            auto place = [&](int gr, int e) { return reinterpret_cast<uint4*>(at0 + (e >> 1) * RW_BLOCK + gr * 2048 + (e & 1) * 1024); };
+#pragma unroll 2
             for (int gr = 0; gr < 8; ++gr) {   // sixteen keys, which lie in one box
-              const int k0 = r.bl.base(c * r.per_chunk + ((gr * 16) >> box_log2)) + ((gr * 16) & ((1 << box_log2) - 1));
-              if (k0 >= r.bl.end) {
-#pragma unroll
-                for (int e = 0; e < 2 * HALVES; ++e)
-                  *reinterpret_cast<uint4*>(at0 + (e >> 1) * RW_BLOCK + gr * 2048 + (e & 1) * 1024) = make_uint4(0u, 0u, 0u, 0u);
-                continue;
-              }
+              const int b0 = it.base(c * per_chunk + ((gr * 16) >> box_log2), box_log2), k0 = b0 + ((gr * 16) & ((1 << box_log2) - 1));
+              if (b0 >= it.end) continue;    // (a box that has not been loaded: zeros)
               uint4 v[2 * HALVES];
 #pragma unroll
-              for (int e = 0; e < 2 * HALVES; ++e) v[e] = *reinterpret_cast<const uint4*>(at0 + (e >> 1) * RW_BLOCK + gr * 2048 + (e & 1) * 1024);
+              for (int e = 0; e < 2 * HALVES; ++e) v[e] = *place(gr, e);
+              auto look = [&](const uint4& x) {
+                bad |= ((x.x & 0x7fff7fffu) + 0x00800080u) | ((x.y & 0x7fff7fffu) + 0x00800080u) | ((x.z & 0x7fff7fffu) + 0x00800080u) |
+                       ((x.w & 0x7fff7fffu) + 0x00800080u);
+              };
+              if (k0 + 16 <= it.end && (k0 + 16 <= it.sinks || k0 >= it.start)) {
 #pragma unroll
-              for (int e = 0; e < 2 * HALVES; ++e) {
-                const int key = k0 + t_key + (e & 1) * 8;
-                if (key >= r.bl.end || (key >= r.bl.sinks && key < r.bl.start)) {
-                  *reinterpret_cast<uint4*>(at0 + (e >> 1) * RW_BLOCK + gr * 2048 + (e & 1) * 1024) = make_uint4(0u, 0u, 0u, 0u);
-                } else {
-                  const uint32_t w[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
+                for (int e = 0; e < 2 * HALVES; ++e) look(v[e]);
+              } else {
 #pragma unroll
-                  for (int j = 0; j < 4; ++j) unclean = unclean || (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
+                for (int e = 0; e < 2 * HALVES; ++e) {
+                  const int key = k0 + t_key + (e & 1) * 8;
+                  if (key >= it.end || (key >= it.sinks && key < it.start)) *place(gr, e) = make_uint4(0u, 0u, 0u, 0u);
+                  else look(v[e]);
                 }
               }
             }
-            if (unclean) s_item[k & 1].unclean = 1;
+            const bool unclean = (bad & 0x80008000u) != 0;
+            if (unclean) *reinterpret_cast<volatile int*>(&s_item[k & 3].unclean) = 1;
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(V_OK + s));
         }
-        g += r.n_chunks;
+        g += it.n_chunks;
         release_item(k);
       }
     }
   } else {
     // ===================== softmax and output: one thread a row =====================
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int tile = (warp - 4) >> 2, w4 = warp & 3;   // (a warp may touch the lane quarter warp mod 4 of tensor memory)
     const int t = w4 * 32 + lane;
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
@@ -436,14 +441,14 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
     const uint64_t scale22 = pair(scale2, scale2);
     // the tile's Q, K-major and swizzled: 16-byte piece c of row r lies at piece c ^ (r & 7) of its 128 bytes.  A tile's Q may be
     // overwritten once the scores of its last chunk have been seen.
-    auto load_q = [&](const RowsItem& it) {
+    auto load_q = [&](const RowsItem& x) {
       constexpr int PIECES = HD / 8, ROWS_PASS = 32 / PIECES;
-      const int piece = lane % PIECES, rows = it.n_rows - tile * RW_TILE;
-      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.a.q) + (long long)(it.row0 + tile * RW_TILE) * p.a.q_stride + (long long)it.head * HD + piece * 8;
+      const int piece = lane % PIECES, rows = x.n_rows - tile * RW_TILE, r0 = w4 * 32 + lane / PIECES;
+      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.a.q) + (long long)(x.row0 + tile * RW_TILE) * p.a.q_stride + (long long)x.head * HD + piece * 8;
       const uint32_t dst = sQ + tile * TILE + (piece >> 3) * RW_BLOCK;
-#pragma unroll
+#pragma unroll 4
       for (int i = 0; i < 32 / ROWS_PASS; ++i) {
-        const int r = w4 * 32 + i * ROWS_PASS + lane / PIECES;
+        const int r = r0 + i * ROWS_PASS;
         cp_async16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), q + (long long)(r < rows ? r : 0) * p.a.q_stride, r < rows);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
@@ -455,35 +460,58 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
       if (lane == 0) mbar_arrive(bar(Q_FULL + tile));
     };
     uint32_t n_s = 0, n_item = 0;   // chunks and items that the tile has worked on
-    RowsItem it;
-    bool ok = next_item(0, it);
-    RowsPlan r;
-    if (ok && it.head >= 0) {
-      r = plan_rows(it, window, sinks, box_log2);
-      if (r.has(tile)) { load_q(it); q_loaded(); }
-    }
-    for (int k = 0; ok && it.head >= 0; ++k) {
+    bool ok = next_item(0), more = ok && s_item[0].head >= 0;
+    if (more && s_item[0].has(tile)) { load_q(s_item[0]); q_loaded(); }
+    for (int k = 0; ok && more; ++k) {
+      const RowsItem& it = s_item[k & 3];
+      const int head = it.head, from = it.from(tile), to = it.to(tile), first = it.first, skew = it.skew;
       const int t_rows = min(RW_TILE, it.n_rows - tile * RW_TILE);   // rows of the tile, <= 0: none
-      const bool valid = t < t_rows, has = r.has(tile);
-      const int pos0 = it.pos0 + tile * RW_TILE, pos1 = pos0 + t_rows - 1;
+      const bool valid = t < t_rows, has = to > from;
+      const int row0 = it.row0 + tile * RW_TILE, pos0 = it.pos0 + tile * RW_TILE;
+      const int all_from = tile ? it.all_from_b : it.all_from, all_to = tile ? it.all_to_b : it.all_to_a;
       const int pos = valid ? pos0 + t : -1, lo = window > 0 ? pos - window + 1 : 0;   // sees [lo, pos] and the sinks
       float m = -INFINITY, l = 0.f;
-      for (int c = r.from(tile); c < r.to(tile); ++c, ++n_s) {
-        bool all = true;   // every row of the tile sees all of the chunk
-        for (int b = 0; b < r.per_chunk; ++b) all = all && r.bl.seen_by_all(c * r.per_chunk + b, pos0, pos1, window);
+      bool next_q = false;
+      auto look_ahead = [&]() {   // what comes next, and its Q on the way
+        if (!next_item(k + 1)) return false;
+        const RowsItem& next = s_item[(k + 1) & 3];
+        more = next.head >= 0;
+        next_q = more && next.has(tile);
+        if (next_q) load_q(next);
+        return true;
+      };
+      for (int c = from; c < to; ++c, ++n_s) {
+        const bool all = c >= all_from && c < all_to;   // every row of the tile sees all of the chunk
         if (!(ok = wait_warp(bar(S_FULL + tile), n_s & 1))) break;
         tc_fence_after();
+        if (c + 1 == to && !(ok = look_ahead())) break;   // the tile's last scores: its Q is free
         float sc[RW_KEYS];
 #pragma unroll
         for (int g = 0; g < RW_KEYS / 32; ++g) tmem_ld32_nowait(s_addr + g * 32, sc + g * 32);
         tmem_ld_wait();
         if (!all) {
+          const int b0 = c << (7 - box_log2);
+          if (b0 >= first) {   // the window's part: one run of keys
+            const int k0 = (b0 + skew) << box_log2, x0 = lo - k0, x1 = pos + 1 - k0, x2 = sinks - k0;
 #pragma unroll
-          for (int g = 0; g < RW_KEYS / 16; ++g) {   // sixteen keys lie in one box
-            const int k0 = r.bl.base(c * r.per_chunk + ((g * 16) >> box_log2)) + ((g * 16) & ((1 << box_log2) - 1));
-            const uint32_t seen = low_bits(pos + 1 - k0) & (~low_bits(lo - k0) | low_bits(sinks - k0));
+            for (int g = 0; g < RW_KEYS / 32; ++g) {
+              const uint32_t seen = low_bits(x1 - 32 * g) & (~low_bits(x0 - 32 * g) | low_bits(x2 - 32 * g));
+              if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sc[g * 16 + j] = ((seen >> j) & 1u) ? sc[g * 16 + j] : -INFINITY;
+              for (int j = 0; j < 32; ++j) sc[g * 32 + j] = ((seen >> j) & 1u) ? sc[g * 32 + j] : -INFINITY;
+            }
+          } else {
+#pragma unroll
+            for (int g = 0; g < RW_KEYS / 32; ++g) {   // sixteen keys lie in one box
+              uint32_t seen = 0;
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int at = g * 32 + e * 16, k0 = it.base(b0 + (at >> box_log2), box_log2) + (at & ((1 << box_log2) - 1));
+                seen |= (low_bits(pos + 1 - k0) & (~low_bits(lo - k0) | low_bits(sinks - k0)) & 0xffffu) << (16 * e);
+              }
+#pragma unroll
+              for (int j = 0; j < 32; ++j) sc[g * 32 + j] = ((seen >> j) & 1u) ? sc[g * 32 + j] : -INFINITY;
+            }
           }
         }
         float mx4[4] = {sc[0], sc[1], sc[2], sc[3]};
@@ -500,15 +528,15 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
           const float corr = !moves ? 1.f : fast_exp2(m - mx);
           if (moves) m = mx;
           l *= corr;
-          if (c > r.from(tile)) {   // the tile's earlier products are complete (its scores were issued behind them)
+          if (c > from) {   // the tile's earlier products are complete (its scores were issued behind them)
 #pragma unroll
-            for (int g = 0; g < HD / 32; ++g) {
-              float ov[32];
-              tmem_ld32_nowait(o_addr + g * 32, ov);
+            for (int g = 0; g < HD / 16; ++g) {   // (sixteen at a time: the row's scores take the registers)
+              uint32_t ov[16];
+              tmem_ld16(o_addr + g * 16, ov);
               tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) ov[j] *= corr;
-              tmem_st32(o_addr + g * 32, ov);
+              for (int j = 0; j < 16; ++j) ov[j] = __float_as_uint(__uint_as_float(ov[j]) * corr);
+              tmem_st16_u32(o_addr + g * 16, ov);
             }
           }
         }
@@ -537,42 +565,42 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
         l += s0 + s1;
       }
       if (!ok) break;
-      // ---- what comes next, its Q on the way while this one's output is finished
-      RowsItem next;
-      if (!(ok = next_item(k + 1, next))) break;
-      RowsPlan rn = r;
-      bool next_q = false;
-      if (next.head >= 0) {
-        rn = plan_rows(next, window, sinks, box_log2);
-        next_q = rn.has(tile);
-        if (next_q) load_q(next);
-      }
+      if (!has && !(ok = look_ahead())) break;
+      if (next_q) q_loaded();   // the next scores are worked on while this output is finished
       if (has && !(ok = wait_warp(bar(O_FULL + tile), n_item & 1))) break;
-      const bool unclean = s_item[k & 1].unclean != 0;
+      const bool unclean = *reinterpret_cast<volatile int*>(&s_item[k & 3].unclean) != 0;
       if (t_rows > 0 && !unclean) {
         tc_fence_after();
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const long long row = it.row0 + tile * RW_TILE + t;
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + row * p.a.out_stride + (long long)it.head * HD;
+        // through shared memory, so that a store covers 128 bytes of each of four rows (16 bytes of 32 rows cost 9000 cycles a tile)
+        uint8_t* mine = gen + (sO - base) + (warp - 4) * RW_STAGE_OUT;
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + (long long)(row0 + w4 * 32) * p.a.out_stride + (long long)head * HD + (lane & 7) * 8;
 #pragma unroll 1
-        for (int g = 0; g < HD / 32; ++g) {
-          float ov[32];
+        for (int g = 0; g < HD / 64; ++g) {
+          float ov[64];
           if (has) {
-            tmem_ld32_nowait(o_addr + g * 32, ov);
+            tmem_ld32_nowait(o_addr + g * 64, ov);
+            tmem_ld32_nowait(o_addr + g * 64 + 32, ov + 32);
             tmem_ld_wait();
           } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) ov[j] = 0.f;
+            for (int j = 0; j < 64; ++j) ov[j] = 0.f;
           }
-          if (valid) {
+          __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              *reinterpret_cast<uint4*>(out + g * 32 + j * 8) =
-                  make_uint4(pack_bf16(ov[j * 8] * inv, ov[j * 8 + 1] * inv), pack_bf16(ov[j * 8 + 2] * inv, ov[j * 8 + 3] * inv),
-                             pack_bf16(ov[j * 8 + 4] * inv, ov[j * 8 + 5] * inv), pack_bf16(ov[j * 8 + 6] * inv, ov[j * 8 + 7] * inv));
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<uint4*>(mine + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                make_uint4(pack_bf16(ov[j * 8] * inv, ov[j * 8 + 1] * inv), pack_bf16(ov[j * 8 + 2] * inv, ov[j * 8 + 3] * inv),
+                           pack_bf16(ov[j * 8 + 4] * inv, ov[j * 8 + 5] * inv), pack_bf16(ov[j * 8 + 6] * inv, ov[j * 8 + 7] * inv));
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + (lane >> 3);
+            if (w4 * 32 + r < t_rows)
+              *reinterpret_cast<uint4*>(out + (long long)r * p.a.out_stride + g * 64) = *reinterpret_cast<const uint4*>(mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
           }
         }
-        if (valid && p.a.lse) p.a.lse[row * p.a.heads + it.head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+        if (valid && p.a.lse) p.a.lse[(long long)(row0 + t) * p.a.heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
       }
       if (has) {
         tc_fence_before();
@@ -580,23 +608,20 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
         if (lane == 0) mbar_arrive(bar(O_EMPTY + tile));
         ++n_item;
       }
-      if (next_q) q_loaded();
       if (t_rows > 0 && unclean) {
         for (int x = w4 * 32; x < min(t_rows, w4 * 32 + 32); ++x) {   // (rare) the warp's rows, one after another
-          const long long row = it.row0 + tile * RW_TILE + x;
+          const long long row = row0 + x;
           float q[HD / 32], o[HD / 32], rm = -INFINITY, rl = 0.f;
 #pragma unroll
           for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
-          load_dims(reinterpret_cast<const __nv_bfloat16*>(p.a.q) + row * p.a.q_stride + (long long)it.head * HD + lane * (HD / 32), q);
+          load_dims(reinterpret_cast<const __nv_bfloat16*>(p.a.q) + row * p.a.q_stride + (long long)head * HD + lane * (HD / 32), q);
           if (pos0 + x >= 0)
-            attend_row_warp<__nv_bfloat16, HD>(pv, p.a.layer, pv.table + (size_t)it.seq * pv.max_pages, it.head / group, pos0 + x, window, sinks, scale2, q,
+            attend_row_warp<__nv_bfloat16, HD>(pv, p.a.layer, pv.table + (size_t)it.seq * pv.max_pages, head / group, pos0 + x, window, sinks, scale2, q,
                                                o, &rm, &rl);
-          store_row_warp<__nv_bfloat16, HD>(p.a, row, it.head, o, rm, rl);
+          store_row_warp<__nv_bfloat16, HD>(p.a, row, head, o, rm, rl);
         }
       }
       release_item(k);
-      it = next;
-      r = rn;
     }
   }
   // ---- everyone meets, then the allocating warp frees the tensor memory
