@@ -17,8 +17,8 @@
 // The CTAs stay (one per SM) and take one item after another, so that the next one's Q, K and V are on their way while the last
 // products and the output of one are finished.
 // Roles: warp 0 finds the items and loads K and V by TMA, warp 1 MMA (the whole warp runs the loop, an elected lane issues), warps
-// 2 and 3 look through V, warps 4-7 softmax A, 8-11 softmax B.  Registers: 384 x 168 = 64,512 at launch; 4 warps go down to 72 and 8 up to 216
-// (128 x 72 + 256 x 216 = 64,512).  Every wait is bounded; on expiry the CTA reports and leaves.
+// 2 and 3 look through V, warps 4-7 softmax A, 8-11 softmax B.  Registers: 384 x 168 = 64,512 at launch; 4 warps go down to 120 and 8 up to 192
+// (128 x 120 + 256 x 192 = 64,512).  Every wait is bounded; on expiry the CTA reports and leaves.
 //
 // Anything may lie in keys that a row does not see.  Scores are masked by selection.  V's rows that no row of the CTA sees are
 // overwritten by zeros, and chunks that only some rows see are looked through: where such a chunk holds NaN or infinities,
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
   };
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
     if (warp == 0) {
       // ===================== producer: what comes next, and K and V by TMA (lane = (box, half) of the chunk) =====================
       const int n = p.rows.n;
@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
     }
   } else {
     // ===================== softmax and output: one thread a row =====================
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     const int tile = (warp - 4) >> 2, w4 = warp & 3;   // (a warp may touch the lane quarter warp mod 4 of tensor memory)
     const int t = w4 * 32 + lane;
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
@@ -490,28 +490,28 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
         for (int g = 0; g < RW_KEYS / 32; ++g) tmem_ld32_nowait(s_addr + g * 32, sc + g * 32);
         tmem_ld_wait();
         if (!all) {
+          uint32_t seen[RW_KEYS / 32];
           const int b0 = c << (7 - box_log2);
           if (b0 >= first) {   // the window's part: one run of keys
             const int k0 = (b0 + skew) << box_log2, x0 = lo - k0, x1 = pos + 1 - k0, x2 = sinks - k0;
 #pragma unroll
-            for (int g = 0; g < RW_KEYS / 32; ++g) {
-              const uint32_t seen = low_bits(x1 - 32 * g) & (~low_bits(x0 - 32 * g) | low_bits(x2 - 32 * g));
-              if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
-#pragma unroll
-              for (int j = 0; j < 32; ++j) sc[g * 32 + j] = ((seen >> j) & 1u) ? sc[g * 32 + j] : -INFINITY;
-            }
+            for (int g = 0; g < RW_KEYS / 32; ++g) seen[g] = low_bits(x1 - 32 * g) & (~low_bits(x0 - 32 * g) | low_bits(x2 - 32 * g));
           } else {
 #pragma unroll
-            for (int g = 0; g < RW_KEYS / 32; ++g) {   // sixteen keys lie in one box
-              uint32_t seen = 0;
+            for (int g = 0; g < RW_KEYS / 32; ++g) seen[g] = 0;
+#pragma unroll 1
+            for (int e = 0; e < RW_KEYS / 16; ++e) {   // sixteen keys lie in one box
+              const int at = e * 16, k0 = it.base(b0 + (at >> box_log2), box_log2) + (at & ((1 << box_log2) - 1));
+              const uint32_t w = (low_bits(pos + 1 - k0) & (~low_bits(lo - k0) | low_bits(sinks - k0)) & 0xffffu) << (16 * (e & 1));
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int at = g * 32 + e * 16, k0 = it.base(b0 + (at >> box_log2), box_log2) + (at & ((1 << box_log2) - 1));
-                seen |= (low_bits(pos + 1 - k0) & (~low_bits(lo - k0) | low_bits(sinks - k0)) & 0xffffu) << (16 * e);
-              }
-#pragma unroll
-              for (int j = 0; j < 32; ++j) sc[g * 32 + j] = ((seen >> j) & 1u) ? sc[g * 32 + j] : -INFINITY;
+              for (int g = 0; g < RW_KEYS / 32; ++g) seen[g] |= g == e >> 1 ? w : 0u;
             }
+          }
+#pragma unroll
+          for (int g = 0; g < RW_KEYS / 32; ++g) {
+            if (__all_sync(0xffffffffu, seen[g] == 0xffffffffu)) continue;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sc[g * 32 + j] = ((seen[g] >> j) & 1u) ? sc[g * 32 + j] : -INFINITY;
           }
         }
         float mx4[4] = {sc[0], sc[1], sc[2], sc[3]};
@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
           if (moves) m = mx;
           l *= corr;
           if (c > from) {   // the tile's earlier products are complete (its scores were issued behind them)
-#pragma unroll
+#pragma unroll 1
             for (int g = 0; g < HD / 16; ++g) {   // (sixteen at a time: the row's scores take the registers)
               uint32_t ov[16];
               tmem_ld16(o_addr + g * 16, ov);
@@ -576,29 +576,32 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
         uint8_t* mine = gen + (sO - base) + (warp - 4) * RW_STAGE_OUT;
         __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + (long long)(row0 + w4 * 32) * p.a.out_stride + (long long)head * HD + (lane & 7) * 8;
 #pragma unroll 1
-        for (int g = 0; g < HD / 64; ++g) {
-          float ov[64];
-          if (has) {
-            tmem_ld32_nowait(o_addr + g * 64, ov);
-            tmem_ld32_nowait(o_addr + g * 64 + 32, ov + 32);
-            tmem_ld_wait();
-          } else {
+        for (int g = 0; g < HD / 64; ++g) {   // (short loops: this code runs once an item, and what it costs is its fetch)
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {
+            uint32_t ov[16];
+            if (has) {
+              tmem_ld16(o_addr + g * 64 + h * 16, ov);
+              tmem_ld_wait();
+            } else {
 #pragma unroll
-            for (int j = 0; j < 64; ++j) ov[j] = 0.f;
+              for (int j = 0; j < 16; ++j) ov[j] = 0u;
+            }
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = pack_bf16(__uint_as_float(ov[2 * j]) * inv, __uint_as_float(ov[2 * j + 1]) * inv);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              *reinterpret_cast<uint4*>(mine + lane * 128 + (((h * 2 + j) ^ (lane & 7)) << 4)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
           }
           __syncwarp();
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<uint4*>(mine + lane * 128 + ((j ^ (lane & 7)) << 4)) =
-                make_uint4(pack_bf16(ov[j * 8] * inv, ov[j * 8 + 1] * inv), pack_bf16(ov[j * 8 + 2] * inv, ov[j * 8 + 3] * inv),
-                           pack_bf16(ov[j * 8 + 4] * inv, ov[j * 8 + 5] * inv), pack_bf16(ov[j * 8 + 6] * inv, ov[j * 8 + 7] * inv));
-          __syncwarp();
-#pragma unroll
+#pragma unroll 4
           for (int i = 0; i < 8; ++i) {
             const int r = i * 4 + (lane >> 3);
             if (w4 * 32 + r < t_rows)
               *reinterpret_cast<uint4*>(out + (long long)r * p.a.out_stride + g * 64) = *reinterpret_cast<const uint4*>(mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
           }
+          __syncwarp();
         }
         if (valid && p.a.lse) p.a.lse[(long long)(row0 + t) * p.a.heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
       }
