@@ -344,8 +344,7 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
         }
         for (int c = 0; c < it.n_chunks && ok; ++c) {
           const uint32_t x = g + c, s = x & 1;
-          if (!(ok = wait_warp(bar(V_OK + s), (x >> 1) & 1))) break;
-          if (c + 1 < it.n_chunks && !(ok = wait_warp(bar(K_FULL + (s ^ 1)), ((x + 1) >> 1) & 1))) break;
+          if (!(ok = wait_warp(bar(V_OK + s), (x >> 1) & 1))) break;   // V, and the next chunk's K
 #pragma unroll
           for (int tile = 0; tile < 2; ++tile) {
             if (it.active(tile, c)) {
@@ -423,7 +422,8 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
             if (unclean) *reinterpret_cast<volatile int*>(&s_item[k & 3].unclean) = 1;
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
-          __syncwarp();
+          // (the next chunk's K is waited for here: the MMA warp has no time to spare)
+          if (c + 1 < it.n_chunks && !(ok = wait_warp(bar(K_FULL + (s ^ 1)), ((x + 1) >> 1) & 1))) break;
           if (lane == 0) mbar_arrive(bar(V_OK + s));
         }
         g += it.n_chunks;
