@@ -10,8 +10,12 @@
 // The most likely tokens (larger logit first, lower index first among equals) need no second pass over the row: the k-th
 // largest of the maxima of 128 groups of threads is a bound that at least k elements reach and, in expectation, few more
 // (k + k^2 / 256 or so); only threads whose own maximum reaches it read their pieces again (from the L2) and list what
-// reaches the bound, and the list is ranked by counting.  Rows with NaN or +inf, and lists that overflow, take one maximum
-// after another instead.
+// reaches the bound, and the list is ranked by counting.  Where fewer than k groups hold anything above -inf, what is above it
+// and the first 1024 elements are listed.  Rows with NaN or +inf, and lists that overflow, take one maximum after another.
+//
+// Bound by memory where there are many rows, if the arithmetic stays short: a thread takes batches of four pieces, with one
+// maximum, one comparison and at most one change of reference a batch, and packed fp32 (5.5 instructions an element; one
+// comparison and two selections for each element's place alone had made it 47).
 #include <cooperative_groups.h>
 
 #include "logprobs.cuh"
@@ -75,18 +79,60 @@ __device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c2) {
   return Sums{r, x.s + y.s, x.u + y.u};
 }
 
-template <int N> __device__ __forceinline__ void add_values(Sums& a, const float (&x)[N], float c2) {
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+typedef float2 f2;
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("{\n\t.reg .b64 w, x, y, z;\n\tmov.b64 w, {%2, %3};\n\tmov.b64 x, {%4, %5};\n\tmov.b64 y, {%6, %7};\n\tfma.rn.f32x2 z, w, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+
+// Adds N values; returns their maximum (NaN left out).
+template <int N> __device__ __forceinline__ float add_values(Sums& a, const float (&x)[N], float c2) {
   float m = x[0];
+  if constexpr (N > 1) {
+    float m2 = x[1];
 #pragma unroll
-  for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+    for (int i = 2; i + 4 <= N; i += 4) { m = max3(m, x[i], x[i + 1]); m2 = max3(m2, x[i + 2], x[i + 3]); }
+    m = max3(m, m2, x[N - 2]);
+    m = fmaxf(m, x[N - 1]);
+  }
   if (m > a.r) a = rebase(a, m, c2);
   const float ref = a.r == -INFINITY ? 0.f : a.r;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float d = (x[i] - ref) * c2, e = ex2(d);
+  if constexpr (N == 1) {
+    const float d = (x[0] - ref) * c2, e = ex2(d);
     a.s += e;
     a.u = fmaf(e, fmaxf(d, -1024.f), a.u);   // (2^-1024 is zero, and 0 * -inf would not be)
+  } else {
+    const f2 nr = make_float2(-ref, -ref), cc = make_float2(c2, c2);
+    f2 s2 = make_float2(a.s, 0.f), u2 = make_float2(a.u, 0.f);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const f2 d = mul2(add2(make_float2(x[i], x[i + 1]), nr), cc);
+      const f2 e = make_float2(ex2(d.x), ex2(d.y));
+      s2 = add2(s2, e);
+      u2 = fma2(e, make_float2(fmaxf(d.x, -1024.f), fmaxf(d.y, -1024.f)), u2);
+    }
+    a.s = s2.x + s2.y; a.u = u2.x + u2.y;
   }
+  return m;
 }
 
 template <typename T>
@@ -95,11 +141,12 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
   using P = Pieces<T>;
   constexpr int N = P::N, UNROLL = 4;
   __shared__ u64 s_best[LP_GROUPS];
+  __shared__ __align__(16) float s_group[LP_GROUPS];
   __shared__ u64 s_list[LP_LIST];
   __shared__ u64 s_top[LOGPROB_MAX_TOP];
   __shared__ Sums s_sums[LP_WARPS];
   __shared__ Sums s_total;
-  __shared__ u64 s_bound;
+  __shared__ float s_bound;
   __shared__ int s_count;
   cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
@@ -136,32 +183,36 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
   const int single = part == 0 ? (t < head ? t : t - head < a.vocab - tail0 ? tail0 + t - head : -1) : -1;   // this thread's single element
   const int step = S * LP_THREADS, p0 = part * LP_THREADS + t;
   Sums sum{-INFINITY, 0.f, 0.f};
-  float best = -INFINITY;
-  int best_at = -1;
-  auto see = [&](float v, int index) {
-    if (v > best || best_at < 0) { best = v; best_at = index; }
-  };
-  for (int p = p0; p < pieces; p += UNROLL * step) {
+  float best = -INFINITY;   // this thread's largest
+  int p = p0;
+  for (; p + (UNROLL - 1) * step < pieces; p += UNROLL * step) {
     uint4 raw[UNROLL];
 #pragma unroll
-    for (int k = 0; k < UNROLL; ++k)
-      if (p + k * step < pieces) raw[k] = body[p + k * step];
+    for (int k = 0; k < UNROLL; ++k) raw[k] = body[p + k * step];
+    if constexpr (N * UNROLL <= 16) {
+      float v[N * UNROLL];
 #pragma unroll
-    for (int k = 0; k < UNROLL; ++k)
-      if (p + k * step < pieces) {
-        float v[N];
+      for (int k = 0; k < UNROLL; ++k) P::unpack(raw[k], v + k * N);
+      best = fmaxf(best, add_values(sum, v, c2));
+    } else {
+#pragma unroll
+      for (int k = 0; k < UNROLL; k += 2) {
+        float v[2 * N];
         P::unpack(raw[k], v);
-        add_values(sum, v, c2);
-#pragma unroll
-        for (int j = 0; j < N; ++j) see(v[j], head + (p + k * step) * N + j);
+        P::unpack(raw[k + 1], v + N);
+        best = fmaxf(best, add_values(sum, v, c2));
       }
+    }
+  }
+  for (; p < pieces; p += step) {
+    float v[N];
+    P::unpack(body[p], v);
+    best = fmaxf(best, add_values(sum, v, c2));
   }
   if (single >= 0) {
     const float v[1] = {to_f<T>(x[single])};
-    add_values(sum, v, c2);
-    if (single < head ? !(best > v[0]) : v[0] > best || best_at < 0) { best = v[0]; best_at = single; }
+    best = fmaxf(best, add_values(sum, v, c2));
   }
-  const u64 mine = best_at >= 0 ? rank_key(best, (uint32_t)best_at) : 0ull;
   // ---- the CTA's sums and the maxima of its groups of four threads
 #pragma unroll
   for (int w = 1; w < 32; w <<= 1) {
@@ -170,13 +221,9 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
   }
   if (lane == 0) s_sums[warp] = sum;
   if (a.top) {
-    u64 g = mine;
-#pragma unroll
-    for (int w = 1; w < 4; w <<= 1) {
-      const u64 o = __shfl_xor_sync(0xffffffffu, g, w);
-      g = o > g ? o : g;
-    }
-    if ((lane & 3) == 0) s_best[t >> 2] = g;
+    float g = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
+    if ((lane & 3) == 0) s_group[t >> 2] = g;
   }
   __syncthreads();
   if (warp == 0) {
@@ -188,31 +235,31 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
     }
     if (lane == 0) s_total = q;
   }
-  if (a.top && t < LP_GROUPS) {   // the group maximum that top - 1 others exceed (equal ones are empty groups)
-    const u64 g = s_best[t];
-    int above = 0, equal_before = 0;
+  if (a.top && t >= LP_THREADS - LP_GROUPS) {   // the group maximum that top - 1 others come before (equal ones in their order)
+    const int mine = t - (LP_THREADS - LP_GROUPS);
+    const float g = s_group[mine];
+    int before = 0;
 #pragma unroll 8
-    for (int j = 0; j < LP_GROUPS; ++j) {
-      const u64 o = s_best[j];
-      above += o > g;
-      equal_before += o == g && j < t;
+    for (int j = 0; j < LP_GROUPS; j += 4) {
+      const float4 o = *reinterpret_cast<const float4*>(&s_group[j]);
+      before += (o.x > g || (o.x == g && j < mine)) + (o.y > g || (o.y == g && j + 1 < mine)) + (o.z > g || (o.z == g && j + 2 < mine)) +
+                (o.w > g || (o.w == g && j + 3 < mine));
     }
-    if (above + equal_before == a.top - 1) s_bound = g;
+    if (before == a.top - 1) s_bound = g;
   }
   __syncthreads();
   if (a.top) {
     const float total = s_total.s;
     bool rounds = total != total;
     if (!rounds) {
-      const u64 bound = s_bound;
+      const float bound = s_bound;
       auto offer = [&](float v, int index) {
-        const u64 key = rank_key(v, (uint32_t)index);
-        if (key >= bound) {
+        if (bound == -INFINITY ? v > bound || index < 1024 : v >= bound) {
           const int place = atomicAdd(&s_count, 1);
-          if (place < LP_LIST) s_list[place] = key;
+          if (place < LP_LIST) s_list[place] = rank_key(v, (uint32_t)index);
         }
       };
-      if (mine >= bound && mine) {
+      if (best >= bound) {
         for (int p = p0; p < pieces; p += UNROLL * step) {
           uint4 raw[UNROLL];
 #pragma unroll
