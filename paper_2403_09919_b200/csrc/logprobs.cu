@@ -46,12 +46,14 @@ __device__ __forceinline__ uint32_t key_index(u64 key) { return 0xffffffffu - (u
 template <typename T> struct Pieces;   // 16 bytes as floats
 template <> struct Pieces<float> {
   static constexpr int N = 4;
+  static __device__ __forceinline__ uint4 nothing() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }   // -inf
   static __device__ __forceinline__ void unpack(const uint4& v, float* x) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
   }
 };
 template <> struct Pieces<__nv_bfloat16> {
   static constexpr int N = 8;
+  static __device__ __forceinline__ uint4 nothing() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
   static __device__ __forceinline__ void unpack(const uint4& v, float* x) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -61,6 +63,7 @@ template <> struct Pieces<__nv_bfloat16> {
 
 // r: largest x so far, s and u relative to it.
 struct Sums { float r, s, u; };
+
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -79,6 +82,19 @@ __device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c2) {
   return Sums{r, x.s + y.s, x.u + y.u};
 }
 
+// Over groups of N lanes: one change of reference each, then plain sums.
+template <int N> __device__ __forceinline__ Sums join_lanes(Sums a, float c2) {
+  float r = a.r;
+#pragma unroll
+  for (int w = 1; w < N; w <<= 1) r = fmaxf(r, __shfl_xor_sync(0xffffffffu, r, w));
+  a = rebase(a, r, c2);
+#pragma unroll
+  for (int w = 1; w < N; w <<= 1) {
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, w);
+    a.u += __shfl_xor_sync(0xffffffffu, a.u, w);
+  }
+  return a;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -147,7 +163,8 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
   __shared__ Sums s_sums[LP_WARPS];
   __shared__ Sums s_total;
   __shared__ float s_bound;
-  __shared__ int s_count;
+  __shared__ int s_count, s_n_who;
+  __shared__ short s_who[LP_THREADS];
   cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
   const int row = blockIdx.x / S, t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -168,13 +185,13 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
   const float c2 = a.inv_t * 1.4426950408889634f;
   float x_token = nan;
   if (part == 0 && t == 0) {
-    s_count = 0;
+    s_count = s_n_who = 0;
     if (a.tokens && a.logprob) {
       const int tok = a.tokens[row];
       if ((unsigned)tok < (unsigned)a.vocab) x_token = to_f<T>(x[tok]);
     }
   } else if (t == 0) {
-    s_count = 0;
+    s_count = s_n_who = 0;
   }
   // the row's elements: single ones up to a 16-byte boundary (head), pieces, single ones behind the last piece
   const int head = min((int)(((16 - ((uintptr_t)x & 15)) & 15) / sizeof(T)), a.vocab);
@@ -184,41 +201,30 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
   const int step = S * LP_THREADS, p0 = part * LP_THREADS + t;
   Sums sum{-INFINITY, 0.f, 0.f};
   float best = -INFINITY;   // this thread's largest
-  int p = p0;
-  for (; p + (UNROLL - 1) * step < pieces; p += UNROLL * step) {
+  for (int p = p0; p < pieces; p += UNROLL * step) {
     uint4 raw[UNROLL];
+    if (p + (UNROLL - 1) * step < pieces) {
 #pragma unroll
-    for (int k = 0; k < UNROLL; ++k) raw[k] = body[p + k * step];
-    if constexpr (N * UNROLL <= 16) {
-      float v[N * UNROLL];
+      for (int k = 0; k < UNROLL; ++k) raw[k] = body[p + k * step];
+    } else {   // the last batch is filled up with -inf
 #pragma unroll
-      for (int k = 0; k < UNROLL; ++k) P::unpack(raw[k], v + k * N);
-      best = fmaxf(best, add_values(sum, v, c2));
-    } else {
-#pragma unroll
-      for (int k = 0; k < UNROLL; k += 2) {
-        float v[2 * N];
-        P::unpack(raw[k], v);
-        P::unpack(raw[k + 1], v + N);
-        best = fmaxf(best, add_values(sum, v, c2));
-      }
+      for (int k = 0; k < UNROLL; ++k) raw[k] = p + k * step < pieces ? body[p + k * step] : P::nothing();
     }
-  }
-  for (; p < pieces; p += step) {
-    float v[N];
-    P::unpack(body[p], v);
-    best = fmaxf(best, add_values(sum, v, c2));
+    constexpr int TAKE = N * UNROLL <= 16 ? UNROLL : 2;   // pieces at a time
+#pragma unroll
+    for (int k = 0; k < UNROLL; k += TAKE) {
+      float v[TAKE * N];
+#pragma unroll
+      for (int i = 0; i < TAKE; ++i) P::unpack(raw[k + i], v + i * N);
+      best = fmaxf(best, add_values(sum, v, c2));
+    }
   }
   if (single >= 0) {
     const float v[1] = {to_f<T>(x[single])};
     best = fmaxf(best, add_values(sum, v, c2));
   }
   // ---- the CTA's sums and the maxima of its groups of four threads
-#pragma unroll
-  for (int w = 1; w < 32; w <<= 1) {
-    const Sums o{__shfl_xor_sync(0xffffffffu, sum.r, w), __shfl_xor_sync(0xffffffffu, sum.s, w), __shfl_xor_sync(0xffffffffu, sum.u, w)};
-    sum = join(sum, o, c2);
-  }
+  sum = join_lanes<32>(sum, c2);
   if (lane == 0) s_sums[warp] = sum;
   if (a.top) {
     float g = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
@@ -228,23 +234,21 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
   __syncthreads();
   if (warp == 0) {
     Sums q = lane < LP_WARPS ? s_sums[lane] : Sums{-INFINITY, 0.f, 0.f};
-#pragma unroll
-    for (int w = 1; w < LP_WARPS; w <<= 1) {
-      const Sums o{__shfl_xor_sync(0xffffffffu, q.r, w), __shfl_xor_sync(0xffffffffu, q.s, w), __shfl_xor_sync(0xffffffffu, q.u, w)};
-      q = join(q, o, c2);
-    }
+    q = join_lanes<LP_WARPS>(q, c2);
     if (lane == 0) s_total = q;
   }
-  if (a.top && t >= LP_THREADS - LP_GROUPS) {   // the group maximum that top - 1 others come before (equal ones in their order)
-    const int mine = t - (LP_THREADS - LP_GROUPS);
+  if (a.top) {   // the group maximum that top - 1 others come before (equal ones in their order): four threads a group
+    const int mine = t >> 2, j0 = (t & 3) * (LP_GROUPS / 4);
     const float g = s_group[mine];
     int before = 0;
-#pragma unroll 8
-    for (int j = 0; j < LP_GROUPS; j += 4) {
-      const float4 o = *reinterpret_cast<const float4*>(&s_group[j]);
-      before += (o.x > g || (o.x == g && j < mine)) + (o.y > g || (o.y == g && j + 1 < mine)) + (o.z > g || (o.z == g && j + 2 < mine)) +
-                (o.w > g || (o.w == g && j + 3 < mine));
+#pragma unroll
+    for (int j = 0; j < LP_GROUPS / 4; j += 4) {
+      const float4 o = *reinterpret_cast<const float4*>(&s_group[j0 + j]);
+      const int d = mine - j0 - j;
+      before += (o.x > g || (o.x == g && d > 0)) + (o.y > g || (o.y == g && d > 1)) + (o.z > g || (o.z == g && d > 2)) + (o.w > g || (o.w == g && d > 3));
     }
+    before += __shfl_xor_sync(0xffffffffu, before, 1);
+    before += __shfl_xor_sync(0xffffffffu, before, 2);
     if (before == a.top - 1) s_bound = g;
   }
   __syncthreads();
@@ -259,23 +263,19 @@ __global__ void __launch_bounds__(LP_THREADS) logprob_kernel(LogprobArgs a) {
           if (place < LP_LIST) s_list[place] = rank_key(v, (uint32_t)index);
         }
       };
-      if (best >= bound) {
-        for (int p = p0; p < pieces; p += UNROLL * step) {
-          uint4 raw[UNROLL];
+      if (best >= bound) s_who[atomicAdd(&s_n_who, 1)] = (short)t;
+      __syncthreads();
+      const int n_who = s_n_who;
+      for (int w = warp; w < n_who; w += LP_WARPS) {   // a warp looks through what one of those threads has read
+        const int who = s_who[w];
+        for (int p = part * LP_THREADS + who + lane * step; p < pieces; p += 32 * step) {
+          float v[N];
+          P::unpack(body[p], v);
 #pragma unroll
-          for (int k = 0; k < UNROLL; ++k)
-            if (p + k * step < pieces) raw[k] = body[p + k * step];
-#pragma unroll
-          for (int k = 0; k < UNROLL; ++k)
-            if (p + k * step < pieces) {
-              float v[N];
-              P::unpack(raw[k], v);
-#pragma unroll
-              for (int j = 0; j < N; ++j) offer(v[j], head + (p + k * step) * N + j);
-            }
+          for (int j = 0; j < N; ++j) offer(v[j], head + p * N + j);
         }
-        if (single >= 0) offer(to_f<T>(x[single]), single);
       }
+      if (single >= 0) offer(to_f<T>(x[single]), single);
       __syncthreads();
       rounds = s_count > LP_LIST;
     }
