@@ -173,6 +173,10 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+# The handle of a device's current stream, without the Stream object around it (3 us a call, as long as a small launch).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class Packed:
     """Caller-owned device buffers of one rd_packed."""
 
@@ -458,6 +462,7 @@ class PagedCache:
         if rc:
             raise RdError(rc, "redrafter_pages_init failed: " + self.L.redrafter_pages_last_error(None).decode())
         self.h = hp
+        self._index = self.device.index
 
     @classmethod
     def empty(cls, n_layers, n_kv_heads, head_dim, page_size, n_pages, max_seqs, max_seq_pages, dtype="bf16", device="cuda:0"):
@@ -485,13 +490,13 @@ class PagedCache:
             raise RdError(rc, self.L.redrafter_pages_last_error(self.h).decode())
 
     def _stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return _raw_stream(self._index)
 
     def _list(self, name, t, n=None):
         """Pointer of a device list of whole numbers (None stays None)."""
         if t is None:
             return None
-        if t.dtype != torch.int32 or t.device != self.device or not t.is_contiguous() or (n is not None and t.numel() != n):
+        if t.dtype != torch.int32 or t.get_device() != self._index or not t.is_contiguous() or (n is not None and t.numel() != n):
             raise ValueError(f"{name}: expected {'a list of' if n is None else n} contiguous int32 on {self.device}")
         return t.data_ptr()
 
@@ -525,46 +530,51 @@ class PagedCache:
         n = self.max_seqs if seqs is None else seqs.numel()
         self._ck(self.L.redrafter_pages_free(self.h, self._list("seqs", seqs), n, self._stream()))
 
-    def _rows(self, name, t, heads):
+    def _rows(self, name, t, shape):
         """Pointer and row stride of rows [n, heads, head_dim] whose heads lie one behind the other."""
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.dtype != self.dtype or t.device != self.device:
-            raise ValueError(f"{name}: expected rows [n, {heads}, {self.head_dim}] of {self.dtype} on {self.device}")
+        if t.shape != shape or t.dtype != self.dtype or t.get_device() != self._index:
+            raise ValueError(f"{name}: expected rows {list(shape)} of {self.dtype} on {self.device}")
         row, head, one = t.stride()
-        if (one != 1 or (head != self.head_dim and heads > 1)) and t.numel():
+        if (one != 1 or (head != shape[2] and shape[1] > 1)) and shape[0]:
             raise ValueError(f"{name}: the heads of a row have to lie one behind the other")
-        return t.data_ptr(), row if t.shape[0] > 1 else max(row, heads * self.head_dim)
-
-    def _entries(self, rows, seqs, row_off):
-        """Number of sequences of a call and the pointers of its lists."""
-        if row_off is not None:
-            n = row_off.numel() - 1
-        else:
-            n = rows
-        return n, self._list("seqs", seqs, n), self._list("row_off", row_off)
+        return t.data_ptr(), row if shape[0] > 1 else max(row, shape[1] * shape[2])
 
     def write(self, layer, k, v, row_off=None, seqs=None, max_rows=None):
         """K and V [rows, kv heads, head dim] of the last tokens of sequences into their pages."""
-        n, sp, op = self._entries(k.shape[0], seqs, row_off)
-        (kp, ks), (vp, vs) = self._rows("k", k, self.n_kv_heads), self._rows("v", v, self.n_kv_heads)
-        if v.shape[0] != k.shape[0]:
-            raise ValueError("k and v have different numbers of rows")
-        self._ck(self.L.redrafter_pages_write(self.h, layer, sp, op, n, k.shape[0], kp, ks, vp, vs, self._stream()))
+        rows = k.shape[0]
+        n = rows if row_off is None else row_off.numel() - 1
+        shape = (rows, self.n_kv_heads, self.head_dim)
+        kp, ks = self._rows("k", k, shape)
+        vp, vs = self._rows("v", v, shape)
+        rc = self.L.redrafter_pages_write(self.h, layer, self._list("seqs", seqs, n), self._list("row_off", row_off), n, rows, kp, ks, vp, vs,
+                                          _raw_stream(self._index))
+        if rc:
+            self._ck(rc)
 
     def attention(self, layer, q, out=None, row_off=None, seqs=None, max_rows=None, window=0, sinks=0, scale=0.0, lse=None):
         """Causal attention of rows q [rows, heads, head dim], the last tokens of sequences, over their pages; returns out.
 
         max_rows: the most rows of any sequence (with row_off; it picks the kernel).  lse: [rows, heads] fp32, filled in."""
-        rows, heads = q.shape[0], q.shape[1]
-        n, sp, op = self._entries(rows, seqs, row_off)
+        shape = q.shape
+        if len(shape) != 3 or shape[2] != self.head_dim:
+            raise ValueError(f"q: expected rows [n, heads, {self.head_dim}]")
+        rows, heads = shape[0], shape[1]
         if out is None:
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        elif out.shape != q.shape:
-            raise ValueError("out and q have different shapes")
-        (qp, qs), (outp, outs) = self._rows("q", q, heads), self._rows("out", out, heads)
-        if lse is not None and (lse.dtype != torch.float32 or lse.device != self.device or not lse.is_contiguous() or lse.numel() != rows * heads):
-            raise ValueError(f"lse: expected contiguous float32 [{rows}, {heads}] on {self.device}")
-        self._ck(self.L.redrafter_pages_attention(self.h, layer, sp, op, n, rows, (max_rows or 0) if row_off is not None else 1, heads, qp, qs,
-                                                  outp, outs, None if lse is None else lse.data_ptr(), scale, window, sinks, self._stream()))
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        qp, qs = self._rows("q", q, shape)
+        op, os_ = self._rows("out", out, shape)
+        if lse is not None:
+            if lse.dtype != torch.float32 or lse.get_device() != self._index or not lse.is_contiguous() or lse.numel() != rows * heads:
+                raise ValueError(f"lse: expected contiguous float32 [{rows}, {heads}] on {self.device}")
+            lse = lse.data_ptr()
+        if row_off is None:
+            n, max_rows = rows, 1
+        else:
+            n, row_off, max_rows = row_off.numel() - 1, self._list("row_off", row_off), max_rows or 0
+        rc = self.L.redrafter_pages_attention(self.h, layer, self._list("seqs", seqs, n), row_off, n, rows, max_rows, heads, qp, qs, op, os_, lse,
+                                              scale, window, sinks, _raw_stream(self._index))
+        if rc:
+            self._ck(rc)
         return out
 
     def poll(self):
@@ -582,11 +592,12 @@ def token_logprobs(logits, tokens=None, top=0, temperature=1.0, rows=None, entro
     if logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise ValueError("logits is [rows, vocab] with a row's elements one behind the other")
     dev = logits.device
-    if dev.index != torch.cuda.current_device():
+    index = logits.get_device()
+    if index != torch.cuda.current_device():
         raise ValueError(f"logits lie on {dev}, which is not the current device")
     n = logits.shape[0] if rows is None else rows.numel()
     for name, t in (("tokens", tokens), ("rows", rows)):
-        if t is not None and (t.dtype != torch.int32 or t.device != dev or not t.is_contiguous() or t.numel() != n):
+        if t is not None and (t.dtype != torch.int32 or t.get_device() != index or not t.is_contiguous() or t.numel() != n):
             raise ValueError(f"{name}: expected {n} contiguous int32 on {dev}")
     got = {}
     if tokens is not None:
@@ -602,7 +613,7 @@ def token_logprobs(logits, tokens=None, top=0, temperature=1.0, rows=None, entro
                    None if rows is None else rows.data_ptr(), None if tokens is None else tokens.data_ptr(), ptr.get("logprob"),
                    ptr.get("entropy"), ptr.get("top_ids"), ptr.get("top_logprobs"))
     L = lib()
-    rc = L.redrafter_token_logprobs(C.byref(a), torch.cuda.current_stream().cuda_stream)
+    rc = L.redrafter_token_logprobs(C.byref(a), _raw_stream(index))
     if rc:
         raise RdError(rc, L.redrafter_token_logprobs_error().decode())
     return got
