@@ -69,9 +69,9 @@ struct PageAttention {
   int heads, layer, window, sinks;   // window 0: every earlier key
   float scale;
 };
-// one token per sequence, bf16
+// one token per sequence
 size_t pages_token_part_bytes(const PageView& pv, int grid);
-cudaError_t pages_token_prepare(int hd);
+cudaError_t pages_token_prepare(const PageView& pv);
 cudaError_t launch_pages_token(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int grid, cudaStream_t st);
 // many rows per sequence, bf16
 cudaError_t pages_rows_prepare(int hd);

@@ -25,7 +25,7 @@ struct rd_pages {
   PageView pv;
   int dtype, device;
   int32_t* scratch;
-  char* parts;      // joins of the attention kernel for single tokens (bf16)
+  char* parts;      // joins of the attention kernel for single tokens
   int grid;         // SMs
   int64_t launches;
   char err[256];
@@ -84,7 +84,7 @@ bool view_shape_ok(const PageView& pv) {
 }
 
 size_t scratch_bytes(const PageView& pv) { return (pages_scratch_ints(pv) * 4 + 255) / 256 * 256; }
-size_t page_workspace(const PageView& pv) { return 256 + scratch_bytes(pv) + (pv.es == 2 ? pages_token_part_bytes(pv, TOKEN_MAX_GRID) : 0); }
+size_t page_workspace(const PageView& pv) { return 256 + scratch_bytes(pv) + pages_token_part_bytes(pv, TOKEN_MAX_GRID); }
 
 // What every call on a handle checks first.
 int enter(rd_pages* h, int n) {
@@ -151,8 +151,8 @@ int redrafter_pages_init(const rd_page_cache* cache, void* workspace, size_t ws_
   h->scratch = (int32_t*)((char*)workspace + 256);
   h->parts = (char*)h->scratch + scratch_bytes(pv);
   cudaError_t e = cudaDeviceGetAttribute(&h->grid, cudaDevAttrMultiProcessorCount, dev);
+  if (h->grid > TOKEN_MAX_GRID) h->grid = TOKEN_MAX_GRID;
   if (e == cudaSuccess && pv.es == 2) {
-    if (h->grid > TOKEN_MAX_GRID) h->grid = TOKEN_MAX_GRID;
     const uint64_t pool_rows = (uint64_t)pv.n_layers * 2 * pv.n_pages * pv.H * pv.ps;
     const uint32_t box = pv.ps < 64 ? pv.ps : 64;
     int rc = tc_make_map_parts(h->map_parts.bytes, pv.pool, pool_rows, pv.hd, box);
@@ -161,10 +161,10 @@ int redrafter_pages_init(const rd_page_cache* cache, void* workspace, size_t ws_
       delete h;
       return init_fail(RD_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d for the pool", rc);
     }
-    e = pages_token_prepare(pv.hd);
-    if (e == cudaSuccess) e = pages_rows_prepare(pv.hd);
-    if (e == cudaSuccess) e = cudaMemsetAsync(h->parts, 0, pages_token_part_bytes(pv, TOKEN_MAX_GRID), 0);
+    e = pages_rows_prepare(pv.hd);
   }
+  if (e == cudaSuccess) e = pages_token_prepare(pv);
+  if (e == cudaSuccess) e = cudaMemsetAsync(h->parts, 0, pages_token_part_bytes(pv, TOKEN_MAX_GRID), 0);
   if (e == cudaSuccess) e = cudaMemsetAsync(workspace, 0, 256, 0);
   if (e == cudaSuccess) e = launch_pages_scratch(h->pv, h->scratch, 0);
   if (e == cudaSuccess) e = cudaStreamSynchronize(0);
@@ -276,7 +276,7 @@ int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, c
   a.q = q; a.out = out; a.lse = lse; a.q_stride = q_stride; a.out_stride = out_stride; a.heads = n_heads; a.layer = layer;
   a.window = window; a.sinks = window ? sinks : 0;
   a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)h->pv.hd);
-  if (h->pv.es == 2 && rows.max_rows == 1) PCK(launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, (cudaStream_t)stream));
+  if (rows.max_rows == 1) PCK(launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, (cudaStream_t)stream));
   else if (h->pv.es == 2) PCK(launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, h->grid, (cudaStream_t)stream));
   else PCK(launch_pages_attention_plain(h->pv, h->dtype, rows, a, (cudaStream_t)stream));
   h->launches++;
@@ -291,7 +291,7 @@ int redrafter_pages_poll(rd_pages* h, void* stream) {
   PCK(cudaStreamSynchronize(st));
   if (v == 0) return RD_OK;
   PCK(cudaMemsetAsync(h->pv.status, 0, sizeof(int32_t), st));
-  if ((v & DEV_ERR_TIMEOUT) && h->pv.es == 2)   // a launch that gave up may have left counters behind
+  if (v & DEV_ERR_TIMEOUT)   // a launch that gave up may have left counters behind
     PCK(cudaMemsetAsync(h->parts, 0, pages_token_part_bytes(h->pv, TOKEN_MAX_GRID), st));
   if (v & DEV_ERR_TIMEOUT) return fail(h, RD_ERR_TIMEOUT, "device status 0x%x: a bounded wait gave up", v);
   if (v & DEV_ERR_CAPACITY) return fail(h, RD_ERR_CAPACITY, "device status 0x%x: too few free pages, a call that extends changed nothing", v);

@@ -1,4 +1,4 @@
-// Attention of one new token per sequence over a cache in pages (bf16): the keys are split evenly over the SMs and the parts
+// Attention of one new token per sequence over a cache in pages: the keys are split evenly over the SMs and the parts
 // joined in the same launch.
 //
 //   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(scale log2(e) q . k_j - m),  m the running maximum
@@ -17,6 +17,8 @@
 //     arrive joins them in the order of the CTAs, so that the result does not depend on who is last.
 // Keys outside the row's sight are masked by selection and their V is replaced by zeros bit by bit: they may hold anything.
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "pages_attention.cuh"
 #include "pdl.cuh"
@@ -85,6 +87,113 @@ __device__ __forceinline__ int first_key(const Span& s, int chunk) {
   return (chunk < s.sink_chunks ? chunk : s.first_chunk + chunk - s.sink_chunks) * TK_KEYS;
 }
 
+// This CTA's part of the line of units (whole CTA).
+struct Share {
+  Cursor first;
+  long long T;       // units of the line
+  int G, n_units;    // CTAs that take part; units of this one
+};
+struct ShareScratch {
+  long long before;            // chunks before the CTA's first entry
+  long long scan[TK_WARPS + 1];
+  int entry, last;             // that entry; whether this CTA joins an item's parts
+};
+
+__device__ __forceinline__ Share share_of(const TokenParams& p, int items, ShareScratch& sc) {
+  Share sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int per = (p.rows.n + TK_THREADS - 1) / TK_THREADS, e0 = min((int)threadIdx.x * per, p.rows.n), e1 = min(e0 + per, p.rows.n);
+  long long mine = 0;
+  for (int i = e0; i < e1; ++i) {
+    int seq, row;
+    mine += span_of(p, i, &seq, &row).chunks;
+  }
+  long long before = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += v;
+  }
+  if (lane == 31) sc.scan[warp] = before;
+  __syncthreads();
+  long long chunks = 0;
+  before -= mine;
+  for (int w = 0; w <= TK_WARPS; ++w) {
+    if (w < warp) before += sc.scan[w];
+    chunks += sc.scan[w];
+  }
+  sh.T = chunks * items;
+  sh.G = (int)min((long long)gridDim.x, (sh.T + TK_MIN_UNITS - 1) / TK_MIN_UNITS);
+  sh.n_units = 0;
+  const int c = blockIdx.x;
+  if (c == 0)   // entries that cannot be answered
+    for (int i = e0; i < e1; ++i) {
+      int first, m;
+      page_rows_of(p.rows, i, &first, &m);
+      if (m > 1 || (m == 1 && page_seq_of(p.pv, p.rows.seqs, i) < 0)) atomicOr(p.pv.status, DEV_ERR_INDEX_RANGE);
+    }
+  if (c >= sh.G) return sh;
+  const long long u0 = sh.T * c / sh.G;
+  sh.n_units = (int)(sh.T * (c + 1) / sh.G - u0);
+  const long long target = u0 / items;   // chunk count at which the CTA's first entry lies
+  if (target >= before && target < before + mine) {
+    int i = e0, seq, row;
+    long long at = before;
+    for (;; ++i) {
+      const int n = span_of(p, i, &seq, &row).chunks;
+      if (target < at + n) break;
+      at += n;
+    }
+    sc.entry = i;
+    sc.before = at;
+  }
+  __syncthreads();
+  sh.first.i = sc.entry;
+  sh.first.s = span_of(p, sh.first.i, &sh.first.seq, &sh.first.row);
+  const int r = (int)(u0 - sc.before * items);   // (units of one entry)
+  sh.first.item = r / sh.first.s.chunks;
+  sh.first.chunk = r - sh.first.item * sh.first.s.chunks;
+  sh.first.item_begin = u0 - sh.first.chunk;
+  return sh;
+}
+
+// An item's CTAs, from its first unit and its chunks.
+__device__ __forceinline__ int cta_of_unit(long long unit, long long T, int G) { return (int)(((unit + 1) * G - 1) / T); }
+
+// The parts of an item joined in the order of its CTAs, by the consumers of the last one to arrive.
+template <typename T, int HD>
+__device__ __forceinline__ void join_parts(const TokenParams& p, int first_cta, int last_cta, int row_out, long long head0, int q_rows) {
+  constexpr int PITCH = HD + 4;
+  const size_t step = (size_t)2 * 16 * PITCH;
+  for (int e = threadIdx.x; e < q_rows * (HD / 4); e += TK_WARPS * 32) {
+    const int row = e / (HD / 4), d = (e - row * (HD / 4)) * 4;
+    const float* at0 = p.parts + ((size_t)first_cta * 2 + 1) * 16 * PITCH + row * PITCH;   // the first CTA's slot 1, the others' slot 0
+    const float* at = p.parts + (size_t)(first_cta + 1) * step + row * PITCH;
+    const int others = last_cta - first_cta;
+    float M = __ldcg(at0 + HD);
+#pragma unroll 8
+    for (int k = 0; k < others; ++k) M = fmaxf(M, __ldcg(at + k * step + HD));
+    const float ref = M == -INFINITY ? 0.f : M;
+    float f = fast_exp2(__ldcg(at0 + HD) - ref);
+    float L = f * __ldcg(at0 + HD + 1);
+    float4 v = __ldcg(reinterpret_cast<const float4*>(at0 + d));
+    v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+#pragma unroll 8
+    for (int k = 0; k < others; ++k) {
+      const float2 st = __ldcg(reinterpret_cast<const float2*>(at + k * step + HD));
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(at + k * step + d));
+      f = fast_exp2(st.x - ref);
+      L = fmaf(f, st.y, L);
+      v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    T* out = reinterpret_cast<T*>(p.a.out) + (long long)row_out * p.a.out_stride + (head0 + row) * HD + d;
+    out[0] = from_f<T>(v.x * inv); out[1] = from_f<T>(v.y * inv); out[2] = from_f<T>(v.z * inv); out[3] = from_f<T>(v.w * inv);
+    if (d == 0 && p.a.lse) p.a.lse[(long long)row_out * p.a.heads + head0 + row] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+  }
+  if (threadIdx.x == 0) p.arrived[first_cta] = 0;
+}
+
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
@@ -97,6 +206,9 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TK_WARPS * 32) : "memory"); }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
                "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
@@ -121,9 +233,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
   uint8_t* misc = reinterpret_cast<uint8_t*>(s_out + (TK_WARPS - 1) * 16 * PITCH);
   const uint32_t bars = smem_u32(misc);   // full, then empty
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 16 * TK_STAGES);
-  long long* s_total = reinterpret_cast<long long*>(misc + 16 * TK_STAGES + 8);   // [1] all chunks, [1] chunks before the CTA's first entry
-  int* s_first = reinterpret_cast<int*>(s_total + 2);                             // [1] that entry, [1] whether this CTA joins
-  long long* s_scan = reinterpret_cast<long long*>(s_first + 2);                  // [TK_WARPS + 1]
+  ShareScratch& share = *reinterpret_cast<ShareScratch*>(misc + 16 * TK_STAGES + 8);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const PageView& pv = p.pv;
   if (threadIdx.x == 0) {
@@ -134,62 +244,12 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
   }
   pdl_enter();
 
-  // ---- the line of units and this CTA's part of it
-  const int items = pv.H * p.tiles;
-  const int per = (p.rows.n + TK_THREADS - 1) / TK_THREADS, e0 = min((int)threadIdx.x * per, p.rows.n), e1 = min(e0 + per, p.rows.n);
-  long long mine = 0;
-  for (int i = e0; i < e1; ++i) {
-    int seq, row;
-    mine += span_of(p, i, &seq, &row).chunks;
-  }
-  long long before = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, before, o);
-    if (lane >= o) before += v;
-  }
-  if (lane == 31) s_scan[warp] = before;
-  __syncthreads();
-  long long chunks = 0;
-  before -= mine;
-  for (int w = 0; w <= TK_WARPS; ++w) {
-    if (w < warp) before += s_scan[w];
-    chunks += s_scan[w];
-  }
-  const long long T = chunks * items;
-  const long long want = (T + TK_MIN_UNITS - 1) / TK_MIN_UNITS;
-  const int G = (int)min((long long)gridDim.x, want), c = blockIdx.x;
-  if (blockIdx.x == 0)   // entries that cannot be answered
-    for (int i = e0; i < e1; ++i) {
-      int first, m;
-      page_rows_of(p.rows, i, &first, &m);
-      if (m > 1 || (m == 1 && page_seq_of(pv, p.rows.seqs, i) < 0)) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
-    }
-  if (c >= G) return;
-  const long long u0 = T * c / G, u1 = T * (c + 1) / G;
-  const long long target = u0 / items;   // chunk count at which the CTA's first entry lies
-  if (target >= before && target < before + mine) {
-    int i = e0, seq, row;
-    long long at = before;
-    for (;; ++i) {
-      const int n = span_of(p, i, &seq, &row).chunks;
-      if (target < at + n) break;
-      at += n;
-    }
-    *s_first = i;
-    s_total[1] = at;
-  }
-  __syncthreads();
-  Cursor cur;
-  cur.i = *s_first;
-  cur.s = span_of(p, cur.i, &cur.seq, &cur.row);
-  {
-    const long long r = u0 - s_total[1] * items;
-    cur.item = (int)(r / cur.s.chunks);
-    cur.chunk = (int)(r - (long long)cur.item * cur.s.chunks);
-    cur.item_begin = u0 - cur.chunk;
-  }
-  const int n_units = (int)(u1 - u0);
+  const int items = pv.H * p.tiles, c = blockIdx.x;
+  const Share sh = share_of(p, items, share);
+  if (sh.n_units == 0) return;
+  Cursor cur = sh.first;
+  const int n_units = sh.n_units, G = sh.G;
+  const long long T = sh.T;
 
   const int box_rows = min(pv.ps, TK_KEYS), boxes = TK_KEYS / box_rows;
   if (warp == TK_WARPS) {
@@ -356,7 +416,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
     }
     consumers_sync();
     const bool whole = todo == item.s.chunks;
-    const int first_cta = whole ? c : (int)(((item.item_begin + 1) * G - 1) / T);
+    const int first_cta = whole ? c : cta_of_unit(item.item_begin, T, G);
     if (warp == 0) {
       float* part = p.parts + ((size_t)c * 2 + (c == first_cta ? 1 : 0)) * 16 * PITCH;   // an item that begins here and goes on: slot 1
 #pragma unroll
@@ -394,47 +454,227 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
     }
     if (!whole) {
       // ---- the last of the item's CTAs joins their parts in order
-      const int last_cta = (int)(((item.item_begin + item.s.chunks) * G - 1) / T);
+      const int last_cta = cta_of_unit(item.item_begin + item.s.chunks - 1, T, G);
       if (warp == 0) {
         __syncwarp();
-        int is_last = 0;
         if (lane == 0) {
           __threadfence();
-          is_last = chain_arrive_count(p.arrived + first_cta) == last_cta - first_cta;
-          s_first[1] = is_last;
+          share.last = chain_arrive_count(p.arrived + first_cta) == last_cta - first_cta;
         }
       }
       consumers_sync();
-      if (s_first[1]) {
-        for (int e = threadIdx.x; e < q_rows * (HD / 4); e += TK_WARPS * 32) {
-          const int row = e / (HD / 4), d = (e - row * (HD / 4)) * 4;
-          const size_t step = (size_t)2 * 16 * PITCH;
-          const float* at0 = p.parts + ((size_t)first_cta * 2 + 1) * 16 * PITCH + row * PITCH;   // the first CTA's slot 1, the others' slot 0
-          const float* at = p.parts + (size_t)(first_cta + 1) * step + row * PITCH;
-          const int others = last_cta - first_cta;
-          float M = __ldcg(at0 + HD);
-#pragma unroll 8
-          for (int k = 0; k < others; ++k) M = fmaxf(M, __ldcg(at + k * step + HD));
-          const float ref = M == -INFINITY ? 0.f : M;
-          float f = fast_exp2(__ldcg(at0 + HD) - ref);
-          float L = f * __ldcg(at0 + HD + 1);
-          float4 v = __ldcg(reinterpret_cast<const float4*>(at0 + d));
-          v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-#pragma unroll 8
-          for (int k = 0; k < others; ++k) {
-            const float2 st = __ldcg(reinterpret_cast<const float2*>(at + k * step + HD));
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(at + k * step + d));
-            f = fast_exp2(st.x - ref);
-            L = fmaf(f, st.y, L);
-            v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
-          }
-          const float inv = L == 0.f ? 0.f : 1.f / L;
-          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + (long long)item.row * p.a.out_stride + (head0 + row) * HD + d;
-          *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
-          if (d == 0 && p.a.lse) p.a.lse[(long long)item.row * p.a.heads + head0 + row] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
-        }
-        if (threadIdx.x == 0) p.arrived[first_cta] = 0;
+      if (share.last) join_parts<__nv_bfloat16, HD>(p, first_cta, last_cta, item.row, head0, q_rows);
+    }
+    if (n < n_units) {
+      cur.chunk += todo - 1;
+      next_unit(p, items, cur);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- fp32
+// The same line of units for the fp32 configuration, on the CUDA cores.  A page's rows of a head are one run of bytes, copied as it
+// is; a warp takes 16 keys of a chunk, two lanes a key for the scores (each half of the dimensions, beginning at a place of its own
+// so that eight lanes read eight different banks' worth), then all lanes the dimensions of the output.
+constexpr int TF_STAGES = 3;
+template <int HD> __host__ __device__ constexpr int token_stage_f32() { return 2 * TK_KEYS * HD * 4; }
+template <int HD, int R> constexpr size_t token_smem_f32() {
+  return 128 + (size_t)TF_STAGES * token_stage_f32<HD>() + (size_t)R * HD * 4 + (size_t)TK_WARPS * 16 * 2 * 4 + (size_t)(TK_WARPS - 1) * R * token_pitch<HD>() * 4 + 256;
+}
+
+// R: most query heads of an item.
+template <int HD, int R>
+__global__ void __launch_bounds__(TK_THREADS, 1) pages_token_f32_kernel(const TokenParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  constexpr int STAGE = token_stage_f32<HD>(), PITCH = token_pitch<HD>(), N = HD / 32, QUADS = HD / 8;   // QUADS: 16-byte pieces of half a row
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 127u) & ~127u;
+  uint8_t* gen = smem_raw + (base - raw);
+  float* s_q = reinterpret_cast<float*>(gen + TF_STAGES * STAGE);      // [R][HD]
+  float* s_stat = s_q + R * HD;                                        // [2][TK_WARPS][16]
+  float* s_out = s_stat + 2 * TK_WARPS * 16;                           // [TK_WARPS - 1][R][PITCH]
+  uint8_t* misc = reinterpret_cast<uint8_t*>(s_out + (TK_WARPS - 1) * R * PITCH);
+  const uint32_t bars = smem_u32(misc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 16 * TF_STAGES);
+  ShareScratch& share = *reinterpret_cast<ShareScratch*>(misc + 16 * TF_STAGES + 8);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const PageView& pv = p.pv;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < TF_STAGES; ++s) { mbar_init(bars + 8u * s, 1); mbar_init(bars + 8u * (TF_STAGES + s), TK_WARPS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  pdl_enter();
+  const int items = pv.H * p.tiles, c = blockIdx.x;
+  const Share sh = share_of(p, items, share);
+  if (sh.n_units == 0) return;
+  Cursor cur = sh.first;
+  const int n_units = sh.n_units, G = sh.G;
+  const long long T = sh.T;
+  const int box_rows = min(pv.ps, TK_KEYS), boxes = TK_KEYS / box_rows;
+  if (warp == TK_WARPS) {
+    bool ok = true;
+    const size_t plane = (size_t)pv.n_pages * pv.H * pv.ps * HD;
+    for (int n = 0; n < n_units; ++n) {
+      const int st = n % TF_STAGES, k0 = first_key(cur.s, cur.chunk) + lane * box_rows, h = cur.item / p.tiles;
+      int page = -1;
+      if (lane < boxes && k0 < cur.s.len && cur.seq >= 0 && !(k0 >= cur.s.sink_end && k0 + box_rows <= cur.s.start)) {
+        page = pv.table[(size_t)cur.seq * pv.max_pages + (k0 >> pv.ps_log2)];
+        if ((unsigned)page >= (unsigned)pv.n_pages) { page = -1; atomicOr(pv.status, DEV_ERR_INDEX_RANGE); }
       }
+      if (n + 1 < n_units) next_unit(p, items, cur);
+      if (n >= TF_STAGES) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (TF_STAGES + st), ((n / TF_STAGES) & 1) ^ 1u, abort_flag, pv.status));
+      if (!ok) break;
+      const uint32_t count = __popc(__ballot_sync(0xffffffffu, page >= 0)), bytes = (uint32_t)(box_rows * HD * 4);
+      if (lane == 0) mbar_expect_tx(bars + 8u * st, count * 2 * bytes);
+      __syncwarp();
+      if (page >= 0) {
+        const float* src = reinterpret_cast<const float*>(pv.pool) + (size_t)p.a.layer * 2 * plane + (((size_t)page * pv.H + h) * pv.ps + (k0 & (pv.ps - 1))) * HD;
+        const uint32_t dst = base + (uint32_t)(st * STAGE) + (uint32_t)lane * bytes;
+        bulk_load(dst, src, bytes, bars + 8u * st);
+        bulk_load(dst + STAGE / 2, src + plane, bytes, bars + 8u * st);
+      }
+    }
+    if (!ok) {
+      const unsigned long long t0 = now_ns();
+      while (now_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+    return;
+  }
+  const float scale2 = p.a.scale * LOG2E;
+  const int key = lane >> 1, half = lane & 1, rot = lane & 7, wkey = warp * 16;
+  bool ok = true;
+  for (int n = 0; n < n_units;) {
+    const Cursor item = cur;
+    const int h = item.item / p.tiles, tile = item.item - h * p.tiles;
+    const int q_rows = min(16, p.group - tile * 16);
+    const int todo = min(item.s.chunks - item.chunk, n_units - n);
+    const long long head0 = (long long)h * p.group + tile * 16;
+    consumers_sync();   // the item before is done with its query rows
+    for (int e = threadIdx.x; e < q_rows * HD; e += TK_WARPS * 32)
+      s_q[e] = reinterpret_cast<const float*>(p.a.q)[(long long)item.row * p.a.q_stride + head0 * HD + e] * scale2;
+    consumers_sync();
+    float o[R][N], m[R], l[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+      for (int d = 0; d < N; ++d) o[r][d] = 0.f;
+    }
+    for (int x = 0; x < todo; ++x, ++n) {
+      const int st = n % TF_STAGES, k0 = first_key(item.s, item.chunk + x) + wkey, j = k0 + key;
+      ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * st, (n / TF_STAGES) & 1, abort_flag, pv.status));
+      if (!ok) break;
+      const bool seen = j < item.s.len && (j >= item.s.start || j < item.s.sink_end);
+      const uint32_t any = __ballot_sync(0xffffffffu, seen);
+      if (any) {
+        const float4* kr = reinterpret_cast<const float4*>(gen + st * STAGE + (size_t)(wkey + key) * HD * 4 + half * HD * 2);
+        float s[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < QUADS; ++i) {
+          const int at = (i + rot) % QUADS;
+          const float4 kv = kr[at];
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            if (r >= q_rows) break;
+            const float4 qv = *reinterpret_cast<const float4*>(s_q + r * HD + half * (HD / 2) + at * 4);
+            s[r] = fmaf(kv.x, qv.x, fmaf(kv.y, qv.y, fmaf(kv.z, qv.z, fmaf(kv.w, qv.w, s[r]))));
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (r >= q_rows) break;
+          s[r] += __shfl_xor_sync(0xffffffffu, s[r], 1);
+          s[r] = seen ? s[r] : -INFINITY;
+          float mx = s[r];
+#pragma unroll
+          for (int w = 2; w < 32; w <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+          const float m_new = fmaxf(m[r], mx), ref = m_new == -INFINITY ? 0.f : m_new, corr = exp2f(m[r] - ref);
+          m[r] = m_new;
+          s[r] = exp2f(s[r] - ref);
+          l[r] = l[r] * corr + (half ? 0.f : s[r]);
+#pragma unroll
+          for (int d = 0; d < N; ++d) o[r][d] *= corr;
+        }
+        const float* vr = reinterpret_cast<const float*>(gen + st * STAGE + STAGE / 2) + (size_t)wkey * HD + lane * N;
+#pragma unroll 4
+        for (int y = 0; y < 16; ++y) {
+          if (!((any >> (2 * y)) & 1u)) continue;   // (what is not seen may be anything)
+          float v[N];
+          load_dims(vr + y * HD, v);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            if (r >= q_rows) break;
+            const float w = __shfl_sync(0xffffffffu, s[r], 2 * y);
+#pragma unroll
+            for (int d = 0; d < N; ++d) o[r][d] = fmaf(w, v[d], o[r][d]);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars + 8u * (TF_STAGES + st));
+    }
+    if (!ok) return;
+    // ---- join the warps
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r >= q_rows) break;
+#pragma unroll
+      for (int w = 1; w < 32; w <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
+      if (lane == 0) {
+        s_stat[warp * 16 + r] = m[r];
+        s_stat[TK_WARPS * 16 + warp * 16 + r] = l[r];
+      }
+      if (warp > 0) {
+#pragma unroll
+        for (int d = 0; d < N; ++d) s_out[((warp - 1) * R + r) * PITCH + lane * N + d] = o[r][d];
+      }
+    }
+    consumers_sync();
+    const bool whole = todo == item.s.chunks;
+    const int first_cta = whole ? c : cta_of_unit(item.item_begin, T, G);
+    if (warp == 0) {
+      float* part = p.parts + ((size_t)c * 2 + (c == first_cta ? 1 : 0)) * 16 * PITCH;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r >= q_rows) break;
+        float M = -INFINITY, L = 0.f, f[TK_WARPS];
+#pragma unroll
+        for (int w = 0; w < TK_WARPS; ++w) M = fmaxf(M, s_stat[w * 16 + r]);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < TK_WARPS; ++w) {
+          f[w] = exp2f(s_stat[w * 16 + r] - ref);
+          L = fmaf(f[w], s_stat[TK_WARPS * 16 + w * 16 + r], L);
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        float* out = reinterpret_cast<float*>(p.a.out) + (long long)item.row * p.a.out_stride + (head0 + r) * HD + lane * N;
+#pragma unroll
+        for (int d = 0; d < N; ++d) {
+          float v = o[r][d] * f[0];
+#pragma unroll
+          for (int w = 1; w < TK_WARPS; ++w) v = fmaf(f[w], s_out[((w - 1) * R + r) * PITCH + lane * N + d], v);
+          if (whole) out[d] = v * inv;
+          else part[r * PITCH + lane * N + d] = v;
+        }
+        if (lane == 0) {
+          if (!whole) { part[r * PITCH + HD] = M; part[r * PITCH + HD + 1] = L; }
+          else if (p.a.lse) p.a.lse[(long long)item.row * p.a.heads + head0 + r] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+        }
+      }
+    }
+    if (!whole) {
+      const int last_cta = cta_of_unit(item.item_begin + item.s.chunks - 1, T, G);
+      if (warp == 0) {
+        __syncwarp();
+        if (lane == 0) {
+          __threadfence();
+          share.last = chain_arrive_count(p.arrived + first_cta) == last_cta - first_cta;
+        }
+      }
+      consumers_sync();
+      if (share.last) join_parts<float, HD>(p, first_cta, last_cta, item.row, head0, q_rows);
     }
     if (n < n_units) {
       cur.chunk += todo - 1;
@@ -449,29 +689,44 @@ size_t pages_token_part_bytes(const PageView& pv, int grid) {
   return ((size_t)grid * 2 * 16 * (pv.hd + 4) * 4 + 255) / 256 * 256 + ((size_t)grid * 4 + 255) / 256 * 256;
 }
 
-template <typename F> static cudaError_t for_token_kernels(int hd, F f) {
+// Calls f(kernel, shared memory) for the kernel of these sizes, or for all of the type and head dimension (group < 0).
+template <typename F> static cudaError_t for_token_kernels(int es, int hd, int group, F f) {
   cudaError_t e = cudaSuccess;
-  if (hd == 64) { e = f(pages_token_kernel<64, false>, token_smem<64>()); return e ? e : f(pages_token_kernel<64, true>, token_smem<64>()); }
-  e = f(pages_token_kernel<128, false>, token_smem<128>());
-  return e ? e : f(pages_token_kernel<128, true>, token_smem<128>());
+  auto pick = [&](bool mine, auto kernel, size_t smem) { if (e == cudaSuccess && (group < 0 || mine)) e = f(kernel, smem); };
+  auto bf16 = [&](auto hd_c) {
+    constexpr int HD = decltype(hd_c)::value;
+    pick(group <= 8, pages_token_kernel<HD, false>, token_smem<HD>());
+    pick(group > 8, pages_token_kernel<HD, true>, token_smem<HD>());
+  };
+  auto fp32 = [&](auto hd_c) {
+    constexpr int HD = decltype(hd_c)::value;
+    pick(group == 1, pages_token_f32_kernel<HD, 1>, token_smem_f32<HD, 1>());
+    pick(group > 1 && group <= 4, pages_token_f32_kernel<HD, 4>, token_smem_f32<HD, 4>());
+    pick(group > 4, pages_token_f32_kernel<HD, 16>, token_smem_f32<HD, 16>());
+  };
+  using C64 = std::integral_constant<int, 64>;
+  using C128 = std::integral_constant<int, 128>;
+  if (es == 2) hd == 64 ? bf16(C64{}) : bf16(C128{});
+  else hd == 64 ? fp32(C64{}) : fp32(C128{});
+  return e;
 }
 
-cudaError_t pages_token_prepare(int hd) {
-  return for_token_kernels(hd, [](auto k, size_t smem) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+cudaError_t pages_token_prepare(const PageView& pv) {
+  return for_token_kernels(pv.es, pv.hd, -1, [](auto k, size_t smem) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
 }
 
-// parts: pages_token_part_bytes, its counters zero.  grid: the SMs.
+// map: the pool's rows in boxes of min(page_size, 64) (bf16).  parts: pages_token_part_bytes, its counters zero.  grid: the SMs.
 cudaError_t launch_pages_token(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int grid, cudaStream_t st) {
   TokenParams p;
   p.pv = pv; p.rows = rows; p.a = a;
   p.group = a.heads / pv.H; p.tiles = (p.group + 15) / 16;
   p.parts = (float*)parts;
   p.arrived = (int32_t*)((char*)parts + ((size_t)grid * 2 * 16 * (pv.hd + 4) * 4 + 255) / 256 * 256);
-  auto go = [&](auto k, size_t smem) { launch_pdl(k, grid, TK_THREADS, smem, st, *(const CUtensorMap*)map, p); };
-  const bool wide = p.group > 8;
-  if (pv.hd == 64) wide ? go(pages_token_kernel<64, true>, token_smem<64>()) : go(pages_token_kernel<64, false>, token_smem<64>());
-  else wide ? go(pages_token_kernel<128, true>, token_smem<128>()) : go(pages_token_kernel<128, false>, token_smem<128>());
-  return cudaGetLastError();
+  return for_token_kernels(pv.es, pv.hd, p.group, [&](auto k, size_t smem) {
+    if constexpr (std::is_invocable_v<decltype(k), CUtensorMap, TokenParams>) launch_pdl(k, grid, TK_THREADS, smem, st, *(const CUtensorMap*)map, p);
+    else launch_pdl(k, grid, TK_THREADS, smem, st, p);
+    return cudaGetLastError();
+  });
 }
 
 }  // namespace rd
