@@ -404,7 +404,7 @@ RD_API int redrafter_pages_free(rd_pages* h, const int32_t* seqs, int32_t n, voi
 /* K and V of new tokens into their pages.  The rows of a call belong to n sequences: rows row_off[i] .. row_off[i + 1] - 1
  * (device [n + 1], ascending) to entry i of the list, or, with row_off == NULL, one row to each (n_rows == n).  They are the
  * LAST tokens of their sequences, in order: with m rows, the first of them is token lens - m (extend first).  n_rows bounds
- * the rows; those from row_off[n] on are not looked at.  k, v: [n_rows][n_kv_heads][head_dim] of the cache's dtype, K after
+ * the rows; those from row_off[n] on are not used.  k, v: [n_rows][n_kv_heads][head_dim] of the cache's dtype, K after
  * the rotary embedding, rows k_stride and v_stride elements apart and on 16-byte boundaries.  A sequence is named once.  Rows
  * that would go into a shared page are left out and reported. */
 RD_API int redrafter_pages_write(rd_pages* h, int32_t layer, const int32_t* seqs, const int32_t* row_off, int32_t n, int32_t n_rows, const void* k,

@@ -462,7 +462,9 @@ constexpr int WRITE_THREADS = 128;
 __global__ void __launch_bounds__(WRITE_THREADS) pages_write_kernel(PageView pv, int layer, PageRows rows, const uint4* __restrict__ k, long long k_stride16,
                                                                     const uint4* __restrict__ v, long long v_stride16) {
   pdl_enter();
-  const int row = blockIdx.x;
+  const int row = blockIdx.x, row16 = pv.hd * pv.es / 16, n16 = pv.H * row16, e = blockIdx.y * WRITE_THREADS + threadIdx.x;
+  uint4 a, b;   // requested before the row's place is looked up
+  if (e < n16) { a = __ldcs(k + row * k_stride16 + e); b = __ldcs(v + row * v_stride16 + e); }
   int i = row, first, m;
   if (rows.row_off) {   // the entry whose rows hold this one: the last whose first row is not behind it
     int lo = 0, hi = rows.n;
@@ -491,13 +493,10 @@ __global__ void __launch_bounds__(WRITE_THREADS) pages_write_kernel(PageView pv,
     if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
     return;
   }
-  const int row16 = pv.hd * pv.es / 16, n16 = pv.H * row16;
-  const int e = blockIdx.y * WRITE_THREADS + threadIdx.x;
   if (e >= n16) return;
   const int h = e / row16, c = e - h * row16;
   const size_t plane16 = (size_t)pv.n_pages * pv.H * pv.ps * row16;
   uint4* dst = reinterpret_cast<uint4*>(pv.pool) + (size_t)layer * 2 * plane16 + (((size_t)page * pv.H + h) * pv.ps + slot) * row16 + c;
-  const uint4 a = k[row * k_stride16 + e], b = v[row * v_stride16 + e];
   dst[0] = a;
   dst[plane16] = b;
 }

@@ -99,6 +99,12 @@ struct ShareScratch {
   int entry, last;             // that entry; whether this CTA joins an item's parts
 };
 
+// a * b / c of counts that mostly fit 32 bits (a 64-bit division costs a few hundred cycles, as much as a look into the cache).
+__device__ __forceinline__ long long mul_div(long long a, int b, long long c) {
+  if (a < (1 << 24) && c < (1 << 24) && b < 256) return (uint32_t)a * (uint32_t)b / (uint32_t)c;
+  return a * b / c;
+}
+
 __device__ __forceinline__ Share share_of(const TokenParams& p, int items, ShareScratch& sc) {
   Share sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -133,9 +139,9 @@ __device__ __forceinline__ Share share_of(const TokenParams& p, int items, Share
       if (m > 1 || (m == 1 && page_seq_of(p.pv, p.rows.seqs, i) < 0)) atomicOr(p.pv.status, DEV_ERR_INDEX_RANGE);
     }
   if (c >= sh.G) return sh;
-  const long long u0 = sh.T * c / sh.G;
-  sh.n_units = (int)(sh.T * (c + 1) / sh.G - u0);
-  const long long target = u0 / items;   // chunk count at which the CTA's first entry lies
+  const long long u0 = mul_div(sh.T, c, sh.G);
+  sh.n_units = (int)(mul_div(sh.T, c + 1, sh.G) - u0);
+  const long long target = mul_div(u0, 1, items);   // chunk count at which the CTA's first entry lies
   if (target >= before && target < before + mine) {
     int i = e0, seq, row;
     long long at = before;
@@ -158,7 +164,44 @@ __device__ __forceinline__ Share share_of(const TokenParams& p, int items, Share
 }
 
 // An item's CTAs, from its first unit and its chunks.
-__device__ __forceinline__ int cta_of_unit(long long unit, long long T, int G) { return (int)(((unit + 1) * G - 1) / T); }
+__device__ __forceinline__ int cta_of_unit(long long unit, long long T, int G) {
+  if (unit < (1 << 23) && T < (1 << 24) && G < 256) return (int)(((uint32_t)(unit + 1) * (uint32_t)G - 1) / (uint32_t)T);
+  return (int)(((unit + 1) * G - 1) / T);
+}
+
+// The warps' outputs (s_out [TK_WARPS][R][HD + 4]), maxima and sums (s_stat) joined into the output, or into this CTA's part of an
+// item that it shares: by all consumers, 4 dimensions a thread.
+template <typename T, int HD, int R>
+__device__ __forceinline__ void join_warps(const TokenParams& p, const float* s_stat, const float* s_out, bool whole, int first_cta, int row_out, long long head0,
+                                           int q_rows) {
+  constexpr int PITCH = HD + 4;
+  const int c = blockIdx.x;
+  float* part = p.parts + ((size_t)c * 2 + (c == first_cta ? 1 : 0)) * 16 * PITCH;   // an item that begins here and goes on: slot 1
+  for (int e = threadIdx.x; e < q_rows * (HD / 4); e += TK_WARPS * 32) {
+    const int row = e / (HD / 4), d = (e - row * (HD / 4)) * 4;
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < TK_WARPS; ++w) M = fmaxf(M, s_stat[w * 16 + row]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < TK_WARPS; ++w) {
+      const float f = fast_exp2(s_stat[w * 16 + row] - ref);
+      const float4 x = *reinterpret_cast<const float4*>(s_out + (w * R + row) * PITCH + d);
+      L = fmaf(f, s_stat[TK_WARPS * 16 + w * 16 + row], L);
+      v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+    }
+    if (whole) {
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      T* out = reinterpret_cast<T*>(p.a.out) + (long long)row_out * p.a.out_stride + (head0 + row) * HD + d;
+      out[0] = from_f<T>(v.x * inv); out[1] = from_f<T>(v.y * inv); out[2] = from_f<T>(v.z * inv); out[3] = from_f<T>(v.w * inv);
+      if (d == 0 && p.a.lse) p.a.lse[(long long)row_out * p.a.heads + head0 + row] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+    } else {
+      *reinterpret_cast<float4*>(part + row * PITCH + d) = v;
+      if (d == 0) *reinterpret_cast<float2*>(part + row * PITCH + HD) = make_float2(M, L);
+    }
+  }
+}
 
 // The parts of an item joined in the order of its CTAs, by the consumers of the last one to arrive.
 template <typename T, int HD>
@@ -194,6 +237,22 @@ __device__ __forceinline__ void join_parts(const TokenParams& p, int first_cta, 
   if (threadIdx.x == 0) p.arrived[first_cta] = 0;
 }
 
+// One box of a chunk of the cursor's item: the page (-1: not in the pool, reported), its first token there.
+struct PageBox {
+  bool wanted;
+  int page, slot;
+};
+__device__ __forceinline__ PageBox page_box(const TokenParams& p, const Cursor& c, int chunk, int box, bool in) {
+  const PageView& pv = p.pv;
+  const int rows = min(pv.ps, TK_KEYS), k0 = first_key(c.s, chunk) + box * rows;
+  PageBox b{in && k0 < c.s.len && c.seq >= 0 && !(k0 >= c.s.sink_end && k0 + rows <= c.s.start), -1, k0 & (pv.ps - 1)};   // (not what lies between the sinks and the window)
+  if (b.wanted) {
+    b.page = pv.table[(size_t)c.seq * pv.max_pages + (k0 >> pv.ps_log2)];
+    if ((unsigned)b.page >= (unsigned)pv.n_pages) { b.page = -1; atomicOr(pv.status, DEV_ERR_INDEX_RANGE); }
+  }
+  return b;
+}
+
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
@@ -218,7 +277,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
 template <int HD> __host__ __device__ constexpr int token_stage_bytes() { return 2 * TK_KEYS * HD * 2; }
 template <int HD> __host__ __device__ constexpr int token_pitch() { return HD + 4; }   // floats of a row of parts; also keeps the joins free of bank conflicts
 template <int HD> constexpr size_t token_smem() {
-  return 1024 + (size_t)TK_STAGES * token_stage_bytes<HD>() + (size_t)TK_WARPS * 16 * 2 * 4 + (size_t)(TK_WARPS - 1) * 16 * token_pitch<HD>() * 4 + 256;
+  return 1024 + (size_t)TK_STAGES * token_stage_bytes<HD>() + (size_t)TK_WARPS * 16 * 2 * 4 + (size_t)TK_WARPS * 16 * token_pitch<HD>() * 4 + 256;
 }
 
 // WIDE: more than 8 query heads in an item (rows 8 to 15 of the tile are in use).
@@ -229,8 +288,8 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
   float* s_stat = reinterpret_cast<float*>(gen + TK_STAGES * STAGE);   // [2][TK_WARPS][16] maxima, sums
-  float* s_out = s_stat + 2 * TK_WARPS * 16;                           // [TK_WARPS - 1][16][PITCH] outputs of warps 1 ..
-  uint8_t* misc = reinterpret_cast<uint8_t*>(s_out + (TK_WARPS - 1) * 16 * PITCH);
+  float* s_out = s_stat + 2 * TK_WARPS * 16;                           // [TK_WARPS][16][PITCH] the warps' outputs
+  uint8_t* misc = reinterpret_cast<uint8_t*>(s_out + TK_WARPS * 16 * PITCH);
   const uint32_t bars = smem_u32(misc);   // full, then empty
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 16 * TK_STAGES);
   ShareScratch& share = *reinterpret_cast<ShareScratch*>(misc + 16 * TK_STAGES + 8);
@@ -253,41 +312,29 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
 
   const int box_rows = min(pv.ps, TK_KEYS), boxes = TK_KEYS / box_rows;
   if (warp == TK_WARPS) {
-    // ===================== producer: lane b fetches box b of the chunk's K and V =====================
+    // ===================== producer =====================
     const long long pool_rows = (long long)pv.n_layers * 2 * pv.n_pages * pv.H * pv.ps, plane_rows = (long long)pv.n_pages * pv.H * pv.ps;
-    constexpr int NOT_WANTED = -2;
-    auto page_of = [&](const Cursor& u, int* slot) {   // page of this lane's box and the box's first token in it
-      const int k0 = first_key(u.s, u.chunk) + lane * box_rows;
-      *slot = k0 & (pv.ps - 1);
-      if (lane >= boxes || k0 >= u.s.len || u.seq < 0) return NOT_WANTED;
-      if (k0 >= u.s.sink_end && k0 + box_rows <= u.s.start) return NOT_WANTED;   // between the sinks and the window
-      const int pg = pv.table[(size_t)u.seq * pv.max_pages + (k0 >> pv.ps_log2)];
-      return (unsigned)pg < (unsigned)pv.n_pages ? pg : -1;
-    };
-    int slot, page = page_of(cur, &slot);
+    const int units = 32 / boxes, u = lane / boxes, box = lane - u * boxes;   // lane = (unit of a group, box): a group's pages in one look
     bool ok = true;
-    for (int n = 0; n < n_units; ++n) {
-      const int st = n % TK_STAGES;
-      const int h = cur.item / p.tiles, pg = page, first = slot;
-      const bool wanted = pg != NOT_WANTED;
-      if (n + 1 < n_units) {   // the next chunk's pages are looked up before this one's stage is waited for
-        next_unit(p, items, cur);
-        page = page_of(cur, &slot);
+    for (int n = 0; n < n_units && ok;) {
+      const int h = cur.item / p.tiles, many = min(min(units, cur.s.chunks - cur.chunk), n_units - n);
+      const PageBox b = page_box(p, cur, cur.chunk + u, box, u < many);
+      for (int x = 0; x < many; ++x, ++n) {
+        const int st = n % TK_STAGES;
+        if (n >= TK_STAGES && !(ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (TK_STAGES + st), ((n / TK_STAGES) & 1) ^ 1u, abort_flag, pv.status)))) break;
+        const bool mine = u == x && b.wanted;
+        const uint32_t count = __popc(__ballot_sync(0xffffffffu, mine));
+        if (lane == 0) mbar_expect_tx(bars + 8u * st, count * (uint32_t)(2 * box_rows * HD * 2));
+        __syncwarp();
+        if (mine) {
+          // (behind the pool's last row the copy fills in zeros)
+          const long long row = b.page >= 0 ? (((long long)p.a.layer * 2 * pv.n_pages + b.page) * pv.H + h) * pv.ps + b.slot : pool_rows;
+          const uint32_t dst = base + (uint32_t)(st * STAGE + box * box_rows * HD * 2);
+          tma_load_3d(dst, &map, bars + 8u * st, 0, (int)row, 0);
+          tma_load_3d(dst + STAGE / 2, &map, bars + 8u * st, 0, (int)(b.page >= 0 ? row + plane_rows : pool_rows), 0);
+        }
       }
-      if (n >= TK_STAGES) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (TK_STAGES + st), ((n / TK_STAGES) & 1) ^ 1u, abort_flag, pv.status));
-      if (!ok) break;
-      const uint32_t count = __popc(__ballot_sync(0xffffffffu, wanted));
-      if (lane == 0) mbar_expect_tx(bars + 8u * st, count * (uint32_t)(2 * box_rows * HD * 2));
-      __syncwarp();
-      if (wanted) {
-        const bool there = pg >= 0;
-        if (!there) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
-        // (behind the pool's last row the copy fills in zeros)
-        const long long row = there ? (((long long)p.a.layer * 2 * pv.n_pages + pg) * pv.H + h) * pv.ps + first : pool_rows;
-        const uint32_t dst = base + (uint32_t)(st * STAGE + lane * box_rows * HD * 2);
-        tma_load_3d(dst, &map, bars + 8u * st, 0, (int)row, 0);
-        tma_load_3d(dst + STAGE / 2, &map, bars + 8u * st, 0, (int)(there ? row + plane_rows : pool_rows), 0);
-      }
+      if (ok && n < n_units) { cur.chunk += many - 1; next_unit(p, items, cur); }
     }
     if (!ok) {   // copies already issued land before the CTA's shared memory is given back
       const unsigned long long t0 = now_ns();
@@ -398,7 +445,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
       if (lane == 0) mbar_arrive(bars + 8u * (TK_STAGES + st));
     }
     if (!ok) return;
-    // ---- join the warps: maxima and sums of all, outputs of warps 1 .. through shared memory
+    // ---- join the warps through shared memory
     consumers_sync();   // the join before has been read
 #pragma unroll
     for (int r = 0; r < (WIDE ? 2 : 1); ++r) {
@@ -408,8 +455,8 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
         s_stat[warp * 16 + g + 8 * r] = m[r];
         s_stat[TK_WARPS * 16 + warp * 16 + g + 8 * r] = l[r];
       }
-      if (warp > 0 && g + 8 * r < q_rows) {
-        float* dst = s_out + ((warp - 1) * 16 + g + 8 * r) * PITCH + 2 * t4;
+      if (g + 8 * r < q_rows) {
+        float* dst = s_out + (warp * 16 + g + 8 * r) * PITCH + 2 * t4;
 #pragma unroll
         for (int d = 0; d < HD / 8; ++d) *reinterpret_cast<float2*>(dst + 8 * d) = make_float2(o[d][2 * r], o[d][2 * r + 1]);
       }
@@ -417,51 +464,12 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
     consumers_sync();
     const bool whole = todo == item.s.chunks;
     const int first_cta = whole ? c : cta_of_unit(item.item_begin, T, G);
-    if (warp == 0) {
-      float* part = p.parts + ((size_t)c * 2 + (c == first_cta ? 1 : 0)) * 16 * PITCH;   // an item that begins here and goes on: slot 1
-#pragma unroll
-      for (int r = 0; r < (WIDE ? 2 : 1); ++r) {
-        const int row = g + 8 * r;
-        if (row >= q_rows) continue;
-        float M = -INFINITY, L = 0.f, f[TK_WARPS];
-#pragma unroll
-        for (int w = 0; w < TK_WARPS; ++w) M = fmaxf(M, s_stat[w * 16 + row]);
-        const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-        for (int w = 0; w < TK_WARPS; ++w) {
-          f[w] = fast_exp2(s_stat[w * 16 + row] - ref);
-          L = fmaf(f[w], s_stat[TK_WARPS * 16 + w * 16 + row], L);
-        }
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        const long long out_row = (long long)item.row;
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + out_row * p.a.out_stride + (head0 + row) * HD + 2 * t4;
-#pragma unroll
-        for (int d = 0; d < HD / 8; ++d) {
-          float2 v = make_float2(o[d][2 * r] * f[0], o[d][2 * r + 1] * f[0]);
-#pragma unroll
-          for (int w = 1; w < TK_WARPS; ++w) {
-            const float2 x = *reinterpret_cast<const float2*>(s_out + ((w - 1) * 16 + row) * PITCH + 8 * d + 2 * t4);
-            v.x = fmaf(f[w], x.x, v.x); v.y = fmaf(f[w], x.y, v.y);
-          }
-          if (whole) *reinterpret_cast<uint32_t*>(out + 8 * d) = pack_bf16(v.x * inv, v.y * inv);
-          else *reinterpret_cast<float2*>(part + row * PITCH + 8 * d + 2 * t4) = v;
-        }
-        if (t4 == 0) {
-          if (!whole) { part[row * PITCH + HD] = M; part[row * PITCH + HD + 1] = L; }
-          else if (p.a.lse) p.a.lse[out_row * p.a.heads + head0 + row] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
-        }
-      }
-    }
+    join_warps<__nv_bfloat16, HD, 16>(p, s_stat, s_out, whole, first_cta, item.row, head0, q_rows);
     if (!whole) {
-      // ---- the last of the item's CTAs joins their parts in order
+      // ---- the last of the item's CTAs joins their parts
       const int last_cta = cta_of_unit(item.item_begin + item.s.chunks - 1, T, G);
-      if (warp == 0) {
-        __syncwarp();
-        if (lane == 0) {
-          __threadfence();
-          share.last = chain_arrive_count(p.arrived + first_cta) == last_cta - first_cta;
-        }
-      }
+      consumers_sync();
+      if (threadIdx.x == 0) share.last = chain_arrive_count(p.arrived + first_cta) == last_cta - first_cta;
       consumers_sync();
       if (share.last) join_parts<__nv_bfloat16, HD>(p, first_cta, last_cta, item.row, head0, q_rows);
     }
@@ -476,23 +484,23 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
 // The same line of units for the fp32 configuration, on the CUDA cores.  A page's rows of a head are one run of bytes, copied as it
 // is; a warp takes 16 keys of a chunk, two lanes a key for the scores (each half of the dimensions, beginning at a place of its own
 // so that eight lanes read eight different banks' worth), then all lanes the dimensions of the output.
-constexpr int TF_STAGES = 3;
+template <int HD, int R> __host__ __device__ constexpr int token_stages_f32() { return HD * R == 2048 ? 2 : 3; }   // (16 query heads of dimension 128: their parts take the room)
 template <int HD> __host__ __device__ constexpr int token_stage_f32() { return 2 * TK_KEYS * HD * 4; }
 template <int HD, int R> constexpr size_t token_smem_f32() {
-  return 128 + (size_t)TF_STAGES * token_stage_f32<HD>() + (size_t)R * HD * 4 + (size_t)TK_WARPS * 16 * 2 * 4 + (size_t)(TK_WARPS - 1) * R * token_pitch<HD>() * 4 + 256;
+  return 128 + (size_t)token_stages_f32<HD, R>() * token_stage_f32<HD>() + (size_t)R * HD * 4 + (size_t)TK_WARPS * 16 * 2 * 4 + (size_t)TK_WARPS * R * token_pitch<HD>() * 4 + 256;
 }
 
 // R: most query heads of an item.
 template <int HD, int R>
 __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_f32_kernel(const TokenParams p) {
   extern __shared__ uint8_t smem_raw[];
-  constexpr int STAGE = token_stage_f32<HD>(), PITCH = token_pitch<HD>(), N = HD / 32, QUADS = HD / 8;   // QUADS: 16-byte pieces of half a row
+  constexpr int TF_STAGES = token_stages_f32<HD, R>(), STAGE = token_stage_f32<HD>(), PITCH = token_pitch<HD>(), N = HD / 32, QUADS = HD / 8;   // QUADS: 16-byte pieces of half a row
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 127u) & ~127u;
   uint8_t* gen = smem_raw + (base - raw);
   float* s_q = reinterpret_cast<float*>(gen + TF_STAGES * STAGE);      // [R][HD]
   float* s_stat = s_q + R * HD;                                        // [2][TK_WARPS][16]
-  float* s_out = s_stat + 2 * TK_WARPS * 16;                           // [TK_WARPS - 1][R][PITCH]
-  uint8_t* misc = reinterpret_cast<uint8_t*>(s_out + (TK_WARPS - 1) * R * PITCH);
+  float* s_out = s_stat + 2 * TK_WARPS * 16;                           // [TK_WARPS][R][PITCH]
+  uint8_t* misc = reinterpret_cast<uint8_t*>(s_out + TK_WARPS * R * PITCH);
   const uint32_t bars = smem_u32(misc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 16 * TF_STAGES);
   ShareScratch& share = *reinterpret_cast<ShareScratch*>(misc + 16 * TF_STAGES + 8);
@@ -514,25 +522,26 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_f32_kernel(const To
   if (warp == TK_WARPS) {
     bool ok = true;
     const size_t plane = (size_t)pv.n_pages * pv.H * pv.ps * HD;
-    for (int n = 0; n < n_units; ++n) {
-      const int st = n % TF_STAGES, k0 = first_key(cur.s, cur.chunk) + lane * box_rows, h = cur.item / p.tiles;
-      int page = -1;
-      if (lane < boxes && k0 < cur.s.len && cur.seq >= 0 && !(k0 >= cur.s.sink_end && k0 + box_rows <= cur.s.start)) {
-        page = pv.table[(size_t)cur.seq * pv.max_pages + (k0 >> pv.ps_log2)];
-        if ((unsigned)page >= (unsigned)pv.n_pages) { page = -1; atomicOr(pv.status, DEV_ERR_INDEX_RANGE); }
+    const int units = 32 / boxes, u = lane / boxes, box = lane - u * boxes;
+    const uint32_t bytes = (uint32_t)(box_rows * HD * 4);
+    for (int n = 0; n < n_units && ok;) {
+      const int h = cur.item / p.tiles, many = min(min(units, cur.s.chunks - cur.chunk), n_units - n);
+      const PageBox b = page_box(p, cur, cur.chunk + u, box, u < many);
+      for (int x = 0; x < many; ++x, ++n) {
+        const int st = n % TF_STAGES;
+        if (n >= TF_STAGES && !(ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (TF_STAGES + st), ((n / TF_STAGES) & 1) ^ 1u, abort_flag, pv.status)))) break;
+        const bool mine = u == x && b.wanted && b.page >= 0;
+        const uint32_t count = __popc(__ballot_sync(0xffffffffu, mine));
+        if (lane == 0) mbar_expect_tx(bars + 8u * st, count * 2 * bytes);
+        __syncwarp();
+        if (mine) {
+          const float* src = reinterpret_cast<const float*>(pv.pool) + (size_t)p.a.layer * 2 * plane + (((size_t)b.page * pv.H + h) * pv.ps + b.slot) * HD;
+          const uint32_t dst = base + (uint32_t)(st * STAGE) + (uint32_t)box * bytes;
+          bulk_load(dst, src, bytes, bars + 8u * st);
+          bulk_load(dst + STAGE / 2, src + plane, bytes, bars + 8u * st);
+        }
       }
-      if (n + 1 < n_units) next_unit(p, items, cur);
-      if (n >= TF_STAGES) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (TF_STAGES + st), ((n / TF_STAGES) & 1) ^ 1u, abort_flag, pv.status));
-      if (!ok) break;
-      const uint32_t count = __popc(__ballot_sync(0xffffffffu, page >= 0)), bytes = (uint32_t)(box_rows * HD * 4);
-      if (lane == 0) mbar_expect_tx(bars + 8u * st, count * 2 * bytes);
-      __syncwarp();
-      if (page >= 0) {
-        const float* src = reinterpret_cast<const float*>(pv.pool) + (size_t)p.a.layer * 2 * plane + (((size_t)page * pv.H + h) * pv.ps + (k0 & (pv.ps - 1))) * HD;
-        const uint32_t dst = base + (uint32_t)(st * STAGE) + (uint32_t)lane * bytes;
-        bulk_load(dst, src, bytes, bars + 8u * st);
-        bulk_load(dst + STAGE / 2, src + plane, bytes, bars + 8u * st);
-      }
+      if (ok && n < n_units) { cur.chunk += many - 1; next_unit(p, items, cur); }
     }
     if (!ok) {
       const unsigned long long t0 = now_ns();
@@ -626,53 +635,17 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_f32_kernel(const To
         s_stat[warp * 16 + r] = m[r];
         s_stat[TK_WARPS * 16 + warp * 16 + r] = l[r];
       }
-      if (warp > 0) {
 #pragma unroll
-        for (int d = 0; d < N; ++d) s_out[((warp - 1) * R + r) * PITCH + lane * N + d] = o[r][d];
-      }
+      for (int d = 0; d < N; ++d) s_out[(warp * R + r) * PITCH + lane * N + d] = o[r][d];
     }
     consumers_sync();
     const bool whole = todo == item.s.chunks;
     const int first_cta = whole ? c : cta_of_unit(item.item_begin, T, G);
-    if (warp == 0) {
-      float* part = p.parts + ((size_t)c * 2 + (c == first_cta ? 1 : 0)) * 16 * PITCH;
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (r >= q_rows) break;
-        float M = -INFINITY, L = 0.f, f[TK_WARPS];
-#pragma unroll
-        for (int w = 0; w < TK_WARPS; ++w) M = fmaxf(M, s_stat[w * 16 + r]);
-        const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-        for (int w = 0; w < TK_WARPS; ++w) {
-          f[w] = exp2f(s_stat[w * 16 + r] - ref);
-          L = fmaf(f[w], s_stat[TK_WARPS * 16 + w * 16 + r], L);
-        }
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        float* out = reinterpret_cast<float*>(p.a.out) + (long long)item.row * p.a.out_stride + (head0 + r) * HD + lane * N;
-#pragma unroll
-        for (int d = 0; d < N; ++d) {
-          float v = o[r][d] * f[0];
-#pragma unroll
-          for (int w = 1; w < TK_WARPS; ++w) v = fmaf(f[w], s_out[((w - 1) * R + r) * PITCH + lane * N + d], v);
-          if (whole) out[d] = v * inv;
-          else part[r * PITCH + lane * N + d] = v;
-        }
-        if (lane == 0) {
-          if (!whole) { part[r * PITCH + HD] = M; part[r * PITCH + HD + 1] = L; }
-          else if (p.a.lse) p.a.lse[(long long)item.row * p.a.heads + head0 + r] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
-        }
-      }
-    }
+    join_warps<float, HD, R>(p, s_stat, s_out, whole, first_cta, item.row, head0, q_rows);
     if (!whole) {
       const int last_cta = cta_of_unit(item.item_begin + item.s.chunks - 1, T, G);
-      if (warp == 0) {
-        __syncwarp();
-        if (lane == 0) {
-          __threadfence();
-          share.last = chain_arrive_count(p.arrived + first_cta) == last_cta - first_cta;
-        }
-      }
+      consumers_sync();
+      if (threadIdx.x == 0) share.last = chain_arrive_count(p.arrived + first_cta) == last_cta - first_cta;
       consumers_sync();
       if (share.last) join_parts<float, HD>(p, first_cta, last_cta, item.row, head0, q_rows);
     }
