@@ -260,6 +260,120 @@ __global__ void __launch_bounds__(EXTEND_THREADS) pages_extend_kernel(PageView p
   if (t == 0) sc.job_count[0] = enough ? base_jobs : 0;
 }
 
+// The same for up to EXTEND_FEW entries, an entry a thread, with what is passed on in registers and shared memory: the chain of
+// dependent looks into global memory (sequence, length, last page, its count) is what such a call costs (8 sequences: 9 us with the
+// kernel above, 4 with this one).
+constexpr int EXTEND_FEW = 256, EXTEND_FOUND = 2048;   // entries; pages whose numbers fit shared memory
+
+__global__ void __launch_bounds__(EXTEND_FEW) pages_extend_few_kernel(PageView pv, const int32_t* __restrict__ seqs, const int32_t* __restrict__ n_new,
+                                                                      int n, int32_t* scratch) {
+  __shared__ int s_seq[EXTEND_FEW], s_found[EXTEND_FOUND];
+  __shared__ int2 s_scan[2][EXTEND_FEW / 32];
+  pdl_enter();
+  const PageScratch sc = page_scratch(pv, scratch);
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, words = (pv.n_pages + 31) >> 5;
+  auto free_word = [&](int w) {
+    if (w >= words) return 0u;
+    const int left = pv.n_pages - w * 32;
+    return pv.free_bits[w] & (left < 32 ? (1u << left) - 1u : 0xffffffffu);
+  };
+  uint32_t bits = free_word(t);   // (on its way while the entries are looked up)
+  auto scan = [&](int2 v, int which, int2* total) {   // exclusive scan over the CTA
+    const int2 own = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int a = __shfl_up_sync(0xffffffffu, v.x, o), b = __shfl_up_sync(0xffffffffu, v.y, o);
+      if (lane >= o) { v.x += a; v.y += b; }
+    }
+    if (lane == 31) s_scan[which][warp] = v;
+    __syncthreads();
+    *total = make_int2(0, 0);
+#pragma unroll
+    for (int w = 0; w < EXTEND_FEW / 32; ++w) {
+      const int2 x = s_scan[which][w];
+      if (w < warp) { v.x += x.x; v.y += x.y; }
+      total->x += x.x; total->y += x.y;
+    }
+    return make_int2(v.x - own.x, v.y - own.y);
+  };
+  const int s = t < n ? page_seq_of(pv, seqs, t) : -1, add = t < n ? n_new[t] : 0;
+  if (seqs) {
+    s_seq[t] = s;
+    __syncthreads();
+  }
+  int len = 0, pages = 0, copies = 0, last = -1;
+  bool ok = s >= 0 && add >= 0, partly = false;
+  if (ok) {
+    len = pv.lens[s];
+    ok = len >= 0 && (long long)len + add <= min((long long)pv.max_pages << pv.ps_log2, 0x7fffffffll);
+    if (seqs)
+      for (int j = 0; j < t; ++j) ok = ok && s_seq[j] != s;   // a sequence named twice: its first entry counts
+    partly = ok && add > 0 && (len & (pv.ps - 1));
+  }
+  int32_t* row = pv.table + (size_t)max(s, 0) * pv.max_pages;
+  int names = 1;
+  if (partly) {
+    last = row[len >> pv.ps_log2];
+    ok = partly = (unsigned)last < (unsigned)pv.n_pages;
+    if (partly) names = pv.refs[last];
+  }
+  // (a page with one name has one writer: only shared ones are counted)
+  const bool shared = partly && names > 1;
+  if (shared) {
+    atomicAdd(&sc.sharers[last], 1);
+    atomicMax(&sc.last_sharer[last], t + 1);
+  }
+  if (__syncthreads_or(shared)) {
+    if (shared) copies = !(sc.sharers[last] >= names && sc.last_sharer[last] == t + 1);
+    __syncthreads();
+    if (shared) { sc.sharers[last] = 0; sc.last_sharer[last] = 0; }
+  }
+  const int held = held_pages(pv, len);
+  if (ok) pages = held_pages(pv, len + add) - held + copies;
+  else if (t < n) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);
+  int2 all;
+  const int2 off = scan(make_int2(pages, copies), 0, &all);
+  const int total = all.x;
+  // the lowest free pages
+  int* found = total <= EXTEND_FOUND ? s_found : sc.found;
+  int have = 0;
+  for (int w0 = 0; w0 < words && have < total; w0 += EXTEND_FEW) {
+    if (w0 > 0) {
+      __syncthreads();   // (the sums of the tile before have been read)
+      bits = free_word(w0 + t);
+    }
+    int2 sum;
+    int rank = have + scan(make_int2(__popc(bits), 0), 1, &sum).x;
+    while (bits && rank < total) {
+      found[rank++] = (w0 + t) * 32 + __ffs(bits) - 1;
+      bits &= bits - 1;
+    }
+    have += sum.x;
+  }
+  const bool enough = have >= total;
+  __syncthreads();
+  if (t == 0) {
+    sc.job_count[0] = enough ? all.y : 0;
+    if (!enough) atomicOr(pv.status, DEV_ERR_CAPACITY);
+  }
+  if (!enough) return;
+  for (int k = t; k < total; k += EXTEND_FEW) {
+    const int p = found[k];
+    atomicAnd(&pv.free_bits[p >> 5], ~(1u << (p & 31)));
+    pv.refs[p] = 1;
+  }
+  if (ok && add > 0) {
+    if (copies) {
+      const int p = found[off.x];
+      atomicSub(&pv.refs[last], 1);
+      row[held - 1] = p;
+      sc.jobs[3 * (size_t)off.y] = last; sc.jobs[3 * (size_t)off.y + 1] = p; sc.jobs[3 * (size_t)off.y + 2] = len & (pv.ps - 1);
+    }
+    for (int k = copies; k < pages; ++k) row[held + k - copies] = found[off.x + k];
+    pv.lens[s] = len + add;
+  }
+}
+
 // The filled rows of shared pages into their writers' copies: one run of rows per (job, layer, K or V, head), 16 bytes a
 // thread and four loads in flight.
 constexpr int COPY_THREADS = 256;
@@ -522,7 +636,8 @@ cudaError_t launch_pages_reset(const PageView& pv, int32_t* scratch, cudaStream_
 }
 
 cudaError_t launch_pages_extend(const PageView& pv, const int32_t* seqs, const int32_t* n_new, int n, int32_t* scratch, int* launches, cudaStream_t st) {
-  launch_pdl(pages_extend_kernel, 1, EXTEND_THREADS, 0, st, pv, seqs, n_new, n, scratch);
+  if (n <= EXTEND_FEW) launch_pdl(pages_extend_few_kernel, 1, EXTEND_FEW, 0, st, pv, seqs, n_new, n, scratch);
+  else launch_pdl(pages_extend_kernel, 1, EXTEND_THREADS, 0, st, pv, seqs, n_new, n, scratch);
   if (cudaError_t e = cudaGetLastError()) return e;
   ++*launches;
   const long long units = (long long)n * pv.n_layers * 2 * pv.H;
