@@ -321,7 +321,8 @@ enum {
   RD_ROUTE_GEMM_SWIGLU = 9,       /* of those on CTA pairs: gate|up with SwiGLU behind it */
   RD_ROUTE_GEMM_QKV = 10,         /* of those on CTA pairs: QKV with rotary embedding and cache write behind it */
   RD_ROUTE_ATT_KEYS_ON_LANES = 11,/* tiles of up to 96 rows on tcgen05, keys on the tensor-memory lanes */
-  RD_ROUTE_COUNT = 12
+  RD_ROUTE_ATT_PAGES = 12,        /* over a cache in pages (redrafter_use_pages) */
+  RD_ROUTE_COUNT = 13
 };
 RD_API int redrafter_route_counts(const rd_handle* h, int64_t* out, int32_t n);
 
@@ -454,6 +455,26 @@ typedef struct {
 } rd_logprobs;
 RD_API int redrafter_token_logprobs(const rd_logprobs* args, void* stream);
 RD_API const char* redrafter_token_logprobs_error(void);   /* why the last one failed */
+
+/* Prompts and autoregressive steps of a handle on a cache in pages: from now on redrafter_prefill and redrafter_ar_step make
+ * room in `pages` (redrafter_pages_extend), write their K and V there and attend over it, with the window and sinks given
+ * (0, 0: every earlier key); the handle's own cache is left alone.  Sequence b of the batch is row seqs[b] of the page table
+ * (device [max_batch], borrowed; NULL: row b).  A prompt's sequences are empty before it; an autoregressive step's hold their
+ * contexts (one that does not is reported by the next redrafter_poll).  Between calls the pages may be forked, trimmed and
+ * freed, the state set to match (redrafter_set_state): sequences that share a prompt run it once.  Contexts are bounded by
+ * max_seq_pages * page_size instead of max_ctx; too few free pages are reported by redrafter_pages_poll, and what the call that
+ * met them computes is not defined.  Speculative calls (draft, pack, verify, accept, step) return STATE meanwhile.
+ * pages == NULL: back to the handle's own cache.  Enqueues nothing.  The pages have to outlive their use.
+ * Errors: UNSUPPORTED (fp32, RD_FLAG_FORCE_SIMT), SHAPE (pages of another model), INVALID_ARG, STATE (another device). */
+RD_API int redrafter_use_pages(rd_handle* h, rd_pages* pages, const int32_t* seqs, int32_t window, int32_t sinks);
+
+/* Log probabilities of the tokens that the handle's last call emitted, under softmax(logits / temperature) of the LLM, with
+ * entropy and the `top` most likely tokens (see redrafter_token_logprobs).  Device buffers, each but the last two may be NULL:
+ * logprob, entropy [B][L+1], top_ids, top_logprobs [B][L+1][top].  Column j of sequence b is its j-th emitted token: after
+ * redrafter_step the accepted tokens and the bonus token, columns 0 .. n_accept[b]; after redrafter_ar_step and
+ * redrafter_prefill (the root) column 0.  The other columns are NaN and -1.  Errors: STATE when the last call was none of these. */
+RD_API int redrafter_last_logprobs(rd_handle* h, void* stream, int32_t top, float temperature, float* logprob, float* entropy, int32_t* top_ids,
+                                   float* top_logprobs);
 
 #ifdef __cplusplus
 }

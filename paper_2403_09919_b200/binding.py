@@ -33,10 +33,10 @@ EXPORTS = ["redrafter_workspace_bytes", "redrafter_kv_bytes", "redrafter_init", 
            "redrafter_pages_last_error", "redrafter_pages_reset", "redrafter_pages_extend", "redrafter_pages_fork",
            "redrafter_pages_compact", "redrafter_pages_trim", "redrafter_pages_free", "redrafter_pages_write",
            "redrafter_pages_attention", "redrafter_pages_poll", "redrafter_pages_launch_count", "redrafter_token_logprobs",
-           "redrafter_token_logprobs_error"]
+           "redrafter_token_logprobs_error", "redrafter_use_pages", "redrafter_last_logprobs"]
 
 ROUTES = ("att_rows16", "att_rows16_shallow", "att_rows64", "att_rows128_tc5", "att_key_split", "att_fp32", "gemm_pairs",
-          "gemm_one_cta", "gemm_simt", "gemm_swiglu", "gemm_qkv", "att_keys_on_lanes")
+          "gemm_one_cta", "gemm_simt", "gemm_swiglu", "gemm_qkv", "att_keys_on_lanes", "att_pages")
 
 
 class RdConfig(C.Structure):
@@ -139,6 +139,8 @@ def lib():
         L.redrafter_pages_poll.argtypes = [vp, vp]
         L.redrafter_pages_launch_count.restype = i64
         L.redrafter_pages_launch_count.argtypes = [vp]
+        L.redrafter_use_pages.argtypes = [vp, vp, vp, i32, i32]
+        L.redrafter_last_logprobs.argtypes = [vp, vp, i32, C.c_float, vp, vp, vp, vp]
         L.redrafter_token_logprobs.argtypes = [C.POINTER(RdLogprobs), vp]
         L.redrafter_token_logprobs_error.restype = C.c_char_p
         L.redrafter_token_logprobs_error.argtypes = []
@@ -345,6 +347,27 @@ class ReDrafter:
         self.B = batch
         if ctx_bound is not None:
             self._ck(self.L.redrafter_set_ctx_bound(self.h, int(ctx_bound)))
+
+    def use_pages(self, cache, seqs=None, window=0, sinks=0):
+        """Prompts and autoregressive steps on a PagedCache (None: on the handle's own cache again); seqs: int32 [max_batch], the
+        page table's row of every sequence of the batch."""
+        if seqs is not None and (seqs.dtype != torch.int32 or seqs.device != self.device or not seqs.is_contiguous() or
+                                 seqs.numel() != self.cfg["max_batch"]):
+            raise ValueError(f"seqs: expected {self.cfg['max_batch']} contiguous int32 on {self.device}")
+        self._ck(self.L.redrafter_use_pages(self.h, cache.h if cache is not None else None, _ptr(seqs), int(window), int(sinks)))
+        self._pages = (cache, seqs)                 # keep them alive
+
+    def last_logprobs(self, top=0, temperature=1.0):
+        """Log probabilities of the tokens that the last prefill, step or ar_step emitted: dict of logprob, entropy [B, L + 1] and
+        top_ids, top_logprobs [B, L + 1, top]."""
+        n = self.Lb + 1
+        f32 = dict(dtype=torch.float32, device=self.device)
+        got = dict(logprob=torch.empty(self.B, n, **f32), entropy=torch.empty(self.B, n, **f32))
+        if top > 0:
+            got.update(top_ids=torch.empty(self.B, n, top, dtype=torch.int32, device=self.device), top_logprobs=torch.empty(self.B, n, top, **f32))
+        self._ck(self.L.redrafter_last_logprobs(self.h, _stream(), top, temperature, _ptr(got["logprob"]), _ptr(got["entropy"]),
+                                                _ptr(got.get("top_ids")), _ptr(got.get("top_logprobs"))))
+        return got
 
     def selftest_wait(self):
         self._ck(self.L.redrafter_selftest_wait(self.h, _stream()))

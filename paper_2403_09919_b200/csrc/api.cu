@@ -12,6 +12,8 @@
 #include <utility>
 #include <vector>
 
+#include "logprobs.cuh"
+#include "pages.cuh"
 #include "rd_internal.cuh"
 
 using namespace rd;
@@ -57,6 +59,8 @@ struct Workspace {
   unsigned int* chain_ctr;  // counters of the launch-to-launch hand-off
   float* att_scratch;
   uint32_t* mask_t;   // [B][NMAX][MW] the pass's tree mask with rows and columns exchanged
+  int32_t *emit_row, *emit_tok;   // [B][L + 1] rows of the logits and tokens of what the last call emitted
+  int32_t* page_new;              // [B] tokens by which the pages in use grow
   unsigned long long* trace;  // [TRACE_SLOTS][8] timestamps of traced projection launches
 };
 
@@ -73,6 +77,8 @@ struct alignas(64) TensorMapBox {  // opaque storage of one CUtensorMap (128 byt
 enum { PROF_GEMM = 0, PROF_ATTN = 1, PROF_NORM = 2, PROF_ROPE = 3, PROF_SWIGLU = 4, PROF_DRAFT_SMALL = 5, PROF_PACK_ACCEPT = 6,
        PROF_MISC = 7, PROF_CLASSES = 8 };
 
+enum { EMITTED_NOTHING = 0, EMITTED_PROMPT = 1, EMITTED_AR = 2, EMITTED_STEP = 3 };   // the call that filled the logits
+
 struct rd_handle {
   rd_config cfg;
   Dims dm;
@@ -87,6 +93,10 @@ struct rd_handle {
   int ctx_bound;  // host-side upper bound of every sequence's context length
   int route_bound;  // the same without the feedback below: kernels are chosen by it, so that results follow from the calls alone
   Sampling sampling;  // how the LLM's tokens are chosen (inv_t = 0: greedy)
+  int emitted;    // what redrafter_last_logprobs is about: EMITTED_*
+  rd_pages* pages = nullptr;   // prompts and autoregressive steps run on them; nullptr: on the handle's own cache
+  const int32_t* page_seqs = nullptr;
+  int page_window = 0, page_sinks = 0;
   int64_t launches;
   int64_t route[RD_ROUTE_COUNT];  // launches per kernel variant (redrafter_route_counts)
   // tensor-core path (bf16): TMA descriptors by base pointer, launch geometry
@@ -241,6 +251,7 @@ void carve(Bump& bp, const Dims& dm, int m_cap, Workspace* w) {
   w->tc_partial = bp.take<float>(dm.dtype == RD_DTYPE_BF16 ? tc_partial_floats(TC_MAX_GRID, tc_pick_mt(m_cap)) : 0);
   w->att_scratch = bp.take<float>(dm.dtype == RD_DTYPE_BF16 ? attn_tc_scratch_floats(ATT_MAX_SPLIT_BLOCKS, 1, dm.hd) : 0);
   w->mask_t = bp.take<uint32_t>(dm.dtype == RD_DTYPE_BF16 ? (size_t)B * dm.NMAX * dm.MW : 0);
+  w->emit_row = bp.take<int32_t>((size_t)B * C); w->emit_tok = bp.take<int32_t>((size_t)B * C); w->page_new = bp.take<int32_t>(B);
   w->trace = bp.take<unsigned long long>((size_t)TRACE_SLOTS * 8);
   bp.take<char>(256);
 }
@@ -653,19 +664,29 @@ int forward_layers(rd_handle* h, const uint32_t* mask, int m_max, int n_seq, int
   RowTables rt{w.row_tok, w.row_seq, w.row_pos, w.row_slot, w.row_ncache, w.row_local, mask, w.m_total};
   CKP(h, PROF_MISC, launch_embed_rope(dm.dtype, h->w.tok_emb, w.row_tok, w.row_pos, w.x, w.rope_tab, dm.d, dm.V, dm.hd, dm.theta,
                                       w.m_total, m_max, w.status, st));
+  // On pages the launches wait for one another's grids: the attention there knows no counters.
+  const bool paged = h->pages != nullptr;
   const AttentionPlan ap = plan_attention(h, mask != nullptr, n_seq, rows_per_seq_max);
   GemmOut g_qkv, g_o, g_gu, g_dn;
   // inside the layer loop every launch hands over to the next through a counter; the launches before
   // and after it use the grid dependency
-  Chain* ch = &h->chain;
-  if (int rc0 = chain_start(h, st)) return rc0;
+  Chain* ch = paged ? nullptr : &h->chain;
+  if (paged) {
+    const PageView& pv = pages_view(h->pages);
+    CK(h, launch_page_growth(w.seq_off, w.row_pos, h->page_seqs, pv.lens, pv.max_seqs, n_seq, w.page_new, w.status, st));
+    int launches = 0;
+    CKRT(h, pages_extend_for(h->pages, h->page_seqs, w.page_new, n_seq, &launches, st));
+    h->launches += launches;
+  } else if (int rc0 = chain_start(h, st)) {
+    return rc0;
+  }
   if (!h->use_tc) {
     if (int rc = layers_simt(h, rt, m_max, ch, st)) return rc;
     CKP(h, PROF_NORM, launch_rmsnorm(dm.dtype, w.x, nullptr, h->w.final_norm, w.hidden_t, w.hidden_f, dm.d, dm.eps, w.m_total, m_max, ch, st));
     h->chain.cut();
     return RD_OK;
   }
-  const bool fused_swiglu = use_fused_swiglu(h, m_max, mask == nullptr), fused_qkv = use_fused_qkv(h, m_max, mask == nullptr);
+  const bool fused_swiglu = use_fused_swiglu(h, m_max, mask == nullptr), fused_qkv = !paged && use_fused_qkv(h, m_max, mask == nullptr);
   for (int l = 0; l < dm.n_layers; ++l) {
     // attention block: (x += down of the previous layer) -> norm -> QKV -> rotary + KV write -> attention -> O
     CKP(h, PROF_NORM, launch_rmsnorm(dm.dtype, w.x, l ? &g_dn : nullptr, h->attn_norm[l], w.a_t, nullptr, dm.d, dm.eps,
@@ -677,10 +698,24 @@ int forward_layers(rd_handle* h, const uint32_t* mask, int m_max, int n_seq, int
     } else {
       rc = gemm(h, w.a_t, dm.d, h->wqkv[l], 3 * dm.d, dm.d, w.m_total, m_max, w.qkv, 3 * dm.d, &g_qkv, ch, st, /*pair=*/1);
       if (rc) return rc;
-      CKP(h, PROF_ROPE, launch_rope_kv(w.qkv, g_qkv, kv_plane_ptr(h, l, 0), kv_plane_ptr(h, l, 1), w.rope_tab, rt, dm,
-                                       m_max, w.status, ch, st));
+      KvPages kp{};
+      void *kc = kv_plane_ptr(h, l, 0), *vc = kv_plane_ptr(h, l, 1);
+      if (paged) {   // the normalised rows have been read: their place takes the rotated Q
+        const PageView& pv = pages_view(h->pages);
+        const size_t plane = (size_t)pv.n_pages * pv.H * pv.ps * pv.hd * pv.es;
+        kp = KvPages{pv.table, h->page_seqs, (__nv_bfloat16*)w.a_t, pv.max_seqs, pv.max_pages, pv.n_pages, pv.ps_log2};
+        kc = (char*)pv.pool + (size_t)(2 * l) * plane; vc = (char*)kc + plane;
+      }
+      CKP(h, PROF_ROPE, launch_rope_kv(w.qkv, g_qkv, kc, vc, w.rope_tab, rt, dm, m_max, w.status, ch, paged ? &kp : nullptr, st));
     }
-    {
+    if (paged) {
+      ProfScope ps(h, 1, 0.0, st);
+      PageAttention a{};
+      a.q = w.a_t; a.out = w.attn_t; a.q_stride = a.out_stride = dm.d; a.heads = dm.H; a.layer = l;
+      a.window = h->page_window; a.sinks = h->page_sinks; a.scale = 1.f / sqrtf((float)dm.hd);
+      h->route[RD_ROUTE_ATT_PAGES]++;
+      CK(h, pages_attention_for(h->pages, PageRows{h->page_seqs, w.seq_off, n_seq, m_max, rows_per_seq_max}, a, st));
+    } else {
       ProfScope ps(h, 1, 0.0, st);
       h->route[ap.kl ? RD_ROUTE_ATT_KEYS_ON_LANES : ap.t5 ? RD_ROUTE_ATT_ROWS128_TC5 : ap.wide ? RD_ROUTE_ATT_ROWS64
                : ap.shallow ? RD_ROUTE_ATT_ROWS16_SHALLOW : RD_ROUTE_ATT_ROWS16]++;
@@ -721,8 +756,16 @@ int forward_layers(rd_handle* h, const uint32_t* mask, int m_max, int n_seq, int
   return RD_OK;
 }
 
+// Tokens that a sequence can hold.
+long long context_room(const rd_handle* h) {
+  if (!h->pages) return h->dm.max_ctx;
+  const PageView& pv = pages_view(h->pages);
+  return (long long)pv.max_pages * pv.ps;
+}
+
 int check_stepable(rd_handle* h, cudaStream_t st) {
   if (!h) return RD_ERR_INVALID_ARG;
+  if (h->pages) return fail(h, RD_ERR_STATE, "pages are in use: speculative steps run on the handle's own cache");
   if (!h->prefilled) return fail(h, RD_ERR_STATE, "no state: call redrafter_prefill or redrafter_set_state first");
   fb_poll(h, st);
   if (h->ctx_bound + h->dm.NMAX > h->dm.max_ctx)
@@ -939,6 +982,7 @@ int redrafter_init(const rd_config* cfg, const rd_weights* wt, void* kv_cache, s
     add_a(w.se_t, R, dm.dr + dm.d);
     if (!ok) return init_fail(h, RD_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d for operand %p", failed_rc, failed_ptr);
   }
+  h->emitted = EMITTED_NOTHING;
   h->prefilled = false; h->batch = dm.B; h->ctx_bound = h->route_bound = 0; h->launches = 0; h->err[0] = 0;
   for (int i = 0; i < RD_ROUTE_COUNT; ++i) h->route[i] = 0;
   h->sampling = Sampling{0.0f, 0u, 0u};
@@ -1010,6 +1054,15 @@ int redrafter_route_counts(const rd_handle* h, int64_t* out, int32_t n) {
   return RD_OK;
 }
 
+// The pages in use can take the batch's sequences and belong to the current device.
+static int check_pages(rd_handle* h, int batch) {
+  if (!h->pages) return RD_OK;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev != pages_device(h->pages)) return fail(h, RD_ERR_STATE, "the pages in use are on another device");
+  if (batch > pages_view(h->pages).max_seqs) return fail(h, RD_ERR_CAPACITY, "%d sequences, the page table has %d", batch, pages_view(h->pages).max_seqs);
+  return RD_OK;
+}
+
 static int set_row_counts(rd_handle* h, cudaStream_t st) {
   CK(h, launch_fill_i32(h->ws.one_b, h->batch, 1, st));
   CK(h, launch_fill_i32(h->ws.one_r, h->batch * h->dm.BW, 1, st));
@@ -1026,11 +1079,13 @@ int redrafter_prefill(rd_handle* h, const int32_t* tokens, const int32_t* prompt
   int longest = 0;
   for (int b = 0; b < batch; ++b) {
     if (prompt_len[b] <= 0 || prompt_len[b] > max_prompt) return fail(h, RD_ERR_INVALID_ARG, "prompt_len[%d] = %d", b, prompt_len[b]);
-    if (prompt_len[b] + dm.NMAX > dm.max_ctx) return fail(h, RD_ERR_CAPACITY, "prompt %d of length %d leaves no room for a step", b, prompt_len[b]);
+    if (h->pages ? prompt_len[b] > context_room(h) : prompt_len[b] + dm.NMAX > dm.max_ctx) return fail(h, RD_ERR_CAPACITY, "prompt %d of length %d leaves no room for a step", b, prompt_len[b]);
     longest = prompt_len[b] > longest ? prompt_len[b] : longest;
   }
   // (the prompt would be baked into the graph, and a replay would leave the host's batch and bound as they are)
   if (capturing(st)) return fail(h, RD_ERR_STATE, "prompts cannot be processed under stream capture");
+  if (int rc0 = check_pages(h, batch)) return rc0;
+  h->emitted = EMITTED_NOTHING;
   h->batch = batch;
   int rc = set_row_counts(h, st);
   if (rc) return rc;
@@ -1084,6 +1139,7 @@ int redrafter_prefill(rd_handle* h, const int32_t* tokens, const int32_t* prompt
   // row b is sequence b's last prompt row: the root is the token at position prompt_len[b]
   CK(h, launch_argmax_rows(w.logits, g, dm.V, w.root, nullptr, w.one_b, batch, h->sampling, nullptr, w.ctx, 0, st));
   h->prefilled = true;
+  h->emitted = EMITTED_PROMPT;
   h->ctx_bound = h->route_bound = longest;
   fb_invalidate(h);
   return RD_OK;
@@ -1113,6 +1169,7 @@ int redrafter_verify(rd_handle* h, const rd_packed* packed, void* stream, int32_
   int rc = check_stepable(h, (cudaStream_t)stream);
   if (rc) return rc;
   if (!packed_ok(packed) || !argmax) return fail(h, RD_ERR_INVALID_ARG, "null packed member or argmax");
+  h->emitted = EMITTED_NOTHING;
   return do_verify(h, *packed, (cudaStream_t)stream, argmax, hidden, logits);
 }
 
@@ -1160,6 +1217,7 @@ int redrafter_step(rd_handle* h, const int32_t* planted_beams, void* stream, con
   if (rc) return rc;
   cudaStream_t st = (cudaStream_t)stream;
   Workspace& w = h->ws;
+  h->emitted = EMITTED_NOTHING;
   rc = do_draft(h, st, w.beams, w.scores);
   if (rc) return rc;
   const int32_t* beams = planted_beams ? planted_beams : w.beams;
@@ -1171,6 +1229,7 @@ int redrafter_step(rd_handle* h, const int32_t* planted_beams, void* stream, con
   CKP(h, PROF_PACK_ACCEPT, launch_accept(h->dm.dtype, beams, w.pk, w.argmax_p, w.hidden_f, w.seq_off, h->kv, w.ctx, w.root, w.h, o, w.n_accept,
                       w.best, w.ctx_prev, h->dm, h->batch, w.status, st));
   h->launches++;
+  h->emitted = EMITTED_STEP;
   fb_advance(h, 1 + h->dm.L, st);
   return RD_OK;
 }
@@ -1179,7 +1238,9 @@ int redrafter_ar_step(rd_handle* h, void* stream, int32_t* token) {
   if (!h) return RD_ERR_INVALID_ARG;
   if (!h->prefilled) return fail(h, RD_ERR_STATE, "no state: call redrafter_prefill or redrafter_set_state first");
   fb_poll(h, (cudaStream_t)stream);
-  if (h->ctx_bound + 1 > h->dm.max_ctx) return fail(h, RD_ERR_CAPACITY, "KV cache full");
+  if (h->ctx_bound + 1 > context_room(h)) return fail(h, RD_ERR_CAPACITY, "KV cache full");
+  if (int rc0 = check_pages(h, h->batch)) return rc0;
+  h->emitted = EMITTED_NOTHING;
   cudaStream_t st = (cudaStream_t)stream;
   Workspace& w = h->ws;
   const Dims& dm = h->dm;
@@ -1193,7 +1254,48 @@ int redrafter_ar_step(rd_handle* h, void* stream, int32_t* token) {
   if (rc) return rc;
   CK(h, launch_argmax_rows(w.logits, g, dm.V, w.argmax_c, nullptr, w.m_total, B, h->sampling, w.row_seq, w.row_pos, 1, st));
   CK(h, launch_ar_finish(w.argmax_c, w.hidden_f, w.ctx, w.root, w.h, token, dm, B, st));
+  h->emitted = EMITTED_AR;
   fb_advance(h, 1, st);
+  return RD_OK;
+}
+
+int redrafter_use_pages(rd_handle* h, rd_pages* pages, const int32_t* seqs, int32_t window, int32_t sinks) {
+  if (!h) return RD_ERR_INVALID_ARG;
+  if (pages) {
+    const PageView& pv = pages_view(pages);
+    const Dims& dm = h->dm;
+    if (!h->use_tc) return fail(h, RD_ERR_UNSUPPORTED, "pages are for bf16 handles on the tensor-core path");
+    if (pv.es != 2 || pv.n_layers != dm.n_layers || pv.H != dm.H || pv.hd != dm.hd)
+      return fail(h, RD_ERR_SHAPE, "pages of %d layers, %d heads of dimension %d and %d-byte elements for a model of %d, %d, %d and bf16", pv.n_layers, pv.H, pv.hd, pv.es,
+                  dm.n_layers, dm.H, dm.hd);
+    if (window < 0 || sinks < 0) return fail(h, RD_ERR_INVALID_ARG, "window %d, sinks %d", window, sinks);
+    if (pages_device(pages) != h->device) return fail(h, RD_ERR_STATE, "the pages are on device %d, the handle on %d", pages_device(pages), h->device);
+  }
+  h->pages = pages;
+  h->page_seqs = pages ? seqs : nullptr;
+  h->page_window = pages ? window : 0;
+  h->page_sinks = pages && window ? sinks : 0;
+  return RD_OK;
+}
+
+int redrafter_last_logprobs(rd_handle* h, void* stream, int32_t top, float temperature, float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs) {
+  if (!h) return RD_ERR_INVALID_ARG;
+  if (h->emitted == EMITTED_NOTHING) return fail(h, RD_ERR_STATE, "no prompt, step or autoregressive step has filled the logits last");
+  const Dims& dm = h->dm;
+  Workspace& w = h->ws;
+  if (top < 0 || top > LOGPROB_MAX_TOP || top > dm.V) return fail(h, RD_ERR_SHAPE, "top %d (at most %d)", top, LOGPROB_MAX_TOP);
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return fail(h, RD_ERR_INVALID_ARG, "temperature %g", (double)temperature);
+  if (top && (!top_ids || !top_logprobs)) return fail(h, RD_ERR_INVALID_ARG, "top_ids or top_logprobs is null");
+  cudaStream_t st = (cudaStream_t)stream;
+  const int B = h->batch;
+  const EmittedRows e{B, dm.L, dm.NMAX, h->emitted == EMITTED_PROMPT ? w.root : h->emitted == EMITTED_AR ? w.argmax_c : nullptr,
+                      w.n_accept, w.best, w.pk.unpack, w.seq_off, w.argmax_p};
+  CK(h, launch_emitted_rows(e, dm.BW, w.emit_row, w.emit_tok, st));
+  LogprobArgs a{};
+  a.logits = w.logits; a.row_stride = dm.V; a.row_index = w.emit_row; a.tokens = w.emit_tok; a.rows = B * (dm.L + 1); a.vocab = dm.V;
+  a.n_logit_rows = dm.B * dm.NMAX; a.top = top; a.inv_t = 1.f / temperature;
+  a.logprob = logprob; a.entropy = entropy; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+  CK(h, launch_logprobs(RD_DTYPE_FP32, a, st));
   return RD_OK;
 }
 
@@ -1222,6 +1324,7 @@ int redrafter_set_state(rd_handle* h, void* stream, const int32_t* ctx, const in
   if (batch <= 0 || batch > h->dm.B) return fail(h, RD_ERR_INVALID_ARG, "batch %d outside [1, %d]", batch, h->dm.B);
   cudaStream_t st = (cudaStream_t)stream;
   h->batch = batch;
+  h->emitted = EMITTED_NOTHING;
   int rc = set_row_counts(h, st);
   if (rc) return rc;
   const size_t B = batch;

@@ -393,9 +393,25 @@ __device__ __forceinline__ void store2(__nv_bfloat16* p, float a, float b) {
   *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(a, b);
 }
 
+// Where a row's K and V go: element of the layer's plane at which the row's head begins, -1: nowhere.
+template <bool PAGED> __device__ __forceinline__ long long kv_row(const Dims& dm, const KvPages& pg, int b, int h, int slot) {
+  if (!PAGED) return slot >= 0 && slot < dm.max_ctx ? (((long long)b * dm.H + h) * dm.max_ctx + slot) * dm.hd : -1ll;
+  const int s = pg.seqs ? pg.seqs[b] : b;
+  if ((unsigned)s >= (unsigned)pg.max_seqs || slot < 0 || (slot >> pg.ps_log2) >= pg.max_pages) return -1ll;
+  const int page = pg.table[(size_t)s * pg.max_pages + (slot >> pg.ps_log2)];
+  if ((unsigned)page >= (unsigned)pg.n_pages) return -1ll;
+  return ((((long long)page * dm.H + h) << pg.ps_log2) + (slot & ((1 << pg.ps_log2) - 1))) * dm.hd;
+}
+// The rotated Q: in place for the attention kernels of the contiguous cache, as bf16 rows for those that read pages.
+template <bool PAGED> __device__ __forceinline__ void store_q2(float* row, const KvPages& pg, int m, int d, int o, float a, float b) {
+  if (PAGED) store2(pg.q + (size_t)m * d + o, a, b);
+  else store2(row + o, a, b);
+}
+
+template <bool PAGED>
 __global__ void __maxnreg__(88) rope_kv_kernel(float* __restrict__ qkv, GemmOut proj, __nv_bfloat16* __restrict__ kc, __nv_bfloat16* __restrict__ vc,
                                                const float2* __restrict__ table, RowTables rt, Dims dm, int* status,
-                                               ChainSync cs) {
+                                               ChainSync cs, KvPages pg) {
   chain_begin(cs);
 #ifdef RD_PROBE_EMPTY_BODIES   // ceiling probe (a build flag, never in the shipped library): keep the hand-off, drop the work
   chain_wait_cta(cs);
@@ -439,16 +455,16 @@ __global__ void __maxnreg__(88) rope_kv_kernel(float* __restrict__ qkv, GemmOut 
       const auto dk1 = gemm_load2<ROPE_FOLD>(sk, stride), dk2 = gemm_load2<ROPE_FOLD>(sk, stride, half);
       const auto dv1 = gemm_load2<ROPE_FOLD>(sv, stride), dv2 = gemm_load2<ROPE_FOLD>(sv, stride, half);
       {
-        const bool slot_ok = slot >= 0 && slot < dm.max_ctx;
-        if (!slot_ok && idx == 0) atomicOr(status, DEV_ERR_CAPACITY);
+        const long long kv = kv_row<PAGED>(dm, pg, b, h, slot);
+        if (kv < 0 && idx == 0) atomicOr(status, PAGED ? DEV_ERR_INDEX_RANGE : DEV_ERR_CAPACITY);
         const float2 q1 = gemm_sum2(sq, stride, dq1), q2 = gemm_sum2(sq, stride, dq2, half);
         const float2 k1 = gemm_sum2(sk, stride, dk1), k2 = gemm_sum2(sk, stride, dk2, half);
         const float2 v1 = gemm_sum2(sv, stride, dv1), v2 = gemm_sum2(sv, stride, dv2, half);
         // the attention kernel reads the rotated Q from the projection's own buffer
-        store2(row + o, q1.x * cs2.x - q2.x * cs2.y, q1.y * cs2.z - q2.y * cs2.w);
-        store2(row + o + half, q2.x * cs2.x + q1.x * cs2.y, q2.y * cs2.z + q1.y * cs2.w);
-        if (slot_ok) {
-          const size_t base = (((size_t)b * dm.H + h) * dm.max_ctx + slot) * hd + i;
+        store_q2<PAGED>(row, pg, m, d, o, q1.x * cs2.x - q2.x * cs2.y, q1.y * cs2.z - q2.y * cs2.w);
+        store_q2<PAGED>(row, pg, m, d, o + half, q2.x * cs2.x + q1.x * cs2.y, q2.y * cs2.z + q1.y * cs2.w);
+        if (kv >= 0) {
+          const size_t base = (size_t)kv + i;
           store2(kc + base, k1.x * cs2.x - k2.x * cs2.y, k1.y * cs2.z - k2.y * cs2.w);
           store2(kc + base + half, k2.x * cs2.x + k1.x * cs2.y, k2.y * cs2.z + k1.y * cs2.w);
           store2(vc + base, v1.x, v1.y);
@@ -462,8 +478,8 @@ __global__ void __maxnreg__(88) rope_kv_kernel(float* __restrict__ qkv, GemmOut 
     if (m < M && active) {
       const GemmRows m_tiles = gemm_m_tiles(proj, M);
       b = rt.seq[m]; slot = rt.slot[m];
-      const bool slot_ok = slot >= 0 && slot < dm.max_ctx;
-      if (!slot_ok && idx == 0) atomicOr(status, DEV_ERR_CAPACITY);
+      const long long kv = kv_row<PAGED>(dm, pg, b, h, slot);
+      if (kv < 0 && idx == 0) atomicOr(status, PAGED ? DEV_ERR_INDEX_RANGE : DEV_ERR_CAPACITY);
       cs2 = *reinterpret_cast<const float4*>(tab);
       const GemmFold fq = gemm_fold_or_none(proj, m_tiles, m, o), fk = gemm_fold_or_none(proj, m_tiles, m, d + o),
                      fv = gemm_fold_or_none(proj, m_tiles, m, 2 * d + o);
@@ -473,10 +489,10 @@ __global__ void __maxnreg__(88) rope_kv_kernel(float* __restrict__ qkv, GemmOut 
       const float2 q1 = gemm_finish2(proj, m_tiles, fq, 0, pq1), q2 = gemm_finish2(proj, m_tiles, fq, half, pq2);
       const float2 k1 = gemm_finish2(proj, m_tiles, fk, 0, pk1), k2 = gemm_finish2(proj, m_tiles, fk, half, pk2);
       const float2 v1 = gemm_finish2(proj, m_tiles, fv, 0, pv1), v2 = gemm_finish2(proj, m_tiles, fv, half, pv2);
-      store2(row + o, q1.x * cs2.x - q2.x * cs2.y, q1.y * cs2.z - q2.y * cs2.w);
-      store2(row + o + half, q2.x * cs2.x + q1.x * cs2.y, q2.y * cs2.z + q1.y * cs2.w);
-      if (slot_ok) {
-        const size_t base = (((size_t)b * dm.H + h) * dm.max_ctx + slot) * hd + i;
+      store_q2<PAGED>(row, pg, m, d, o, q1.x * cs2.x - q2.x * cs2.y, q1.y * cs2.z - q2.y * cs2.w);
+      store_q2<PAGED>(row, pg, m, d, o + half, q2.x * cs2.x + q1.x * cs2.y, q2.y * cs2.z + q1.y * cs2.w);
+      if (kv >= 0) {
+        const size_t base = (size_t)kv + i;
         store2(kc + base, k1.x * cs2.x - k2.x * cs2.y, k1.y * cs2.z - k2.y * cs2.w);
         store2(kc + base + half, k2.x * cs2.x + k1.x * cs2.y, k2.y * cs2.z + k1.y * cs2.w);
         store2(vc + base, v1.x, v1.y);
@@ -495,9 +511,10 @@ __global__ void __maxnreg__(88) rope_kv_kernel(float* __restrict__ qkv, GemmOut 
 constexpr int ROPW_THREADS = 256;
 constexpr int ROPW_COLS = 1024;     // one item (two adjacent dimensions and their partners half a head on) per thread
 constexpr int ROPW_STAGES = 3;      // 3 x 3 x 4 KB per CTA (static shared memory)
+template <bool PAGED>
 __global__ void __launch_bounds__(ROPW_THREADS, 4)
     rope_kv_wide_kernel(float* __restrict__ qkv, GemmOut proj, __nv_bfloat16* __restrict__ kc, __nv_bfloat16* __restrict__ vc,
-                        const float2* __restrict__ table, RowTables rt, Dims dm, int* status, ChainSync cs) {
+                        const float2* __restrict__ table, RowTables rt, Dims dm, int* status, ChainSync cs, KvPages pg) {
   chain_begin(cs);
   __shared__ __align__(128) float ring[ROPW_STAGES][3][ROPW_COLS];   // 36 KB
   __shared__ __align__(8) unsigned long long bars[ROPW_STAGES];
@@ -579,14 +596,14 @@ __global__ void __launch_bounds__(ROPW_THREADS, 4)
             v1[part].x += t1.x; v1[part].y += t1.y; v2[part].x += t2.x; v2[part].y += t2.y;
           }
       }
-      const bool slot_ok = slot >= 0 && slot < dm.max_ctx;
-      if (!slot_ok && i == 0 && h == 0) atomicOr(status, DEV_ERR_CAPACITY);
+      const long long kv = kv_row<PAGED>(dm, pg, b, h, slot);
+      if (kv < 0 && i == 0 && h == 0) atomicOr(status, PAGED ? DEV_ERR_INDEX_RANGE : DEV_ERR_CAPACITY);
       // the attention kernel reads the rotated Q from the projection's own buffer
       float* row = qkv + (size_t)m * 3 * d;
-      store2(row + o, v1[0].x * cs2.x - v2[0].x * cs2.y, v1[0].y * cs2.z - v2[0].y * cs2.w);
-      store2(row + o + half, v2[0].x * cs2.x + v1[0].x * cs2.y, v2[0].y * cs2.z + v1[0].y * cs2.w);
-      if (slot_ok) {
-        const size_t base = (((size_t)b * dm.H + h) * dm.max_ctx + slot) * hd + i;
+      store_q2<PAGED>(row, pg, m, d, o, v1[0].x * cs2.x - v2[0].x * cs2.y, v1[0].y * cs2.z - v2[0].y * cs2.w);
+      store_q2<PAGED>(row, pg, m, d, o + half, v2[0].x * cs2.x + v1[0].x * cs2.y, v2[0].y * cs2.z + v1[0].y * cs2.w);
+      if (kv >= 0) {
+        const size_t base = (size_t)kv + i;
         store2(kc + base, v1[1].x * cs2.x - v2[1].x * cs2.y, v1[1].y * cs2.z - v2[1].y * cs2.w);
         store2(kc + base + half, v2[1].x * cs2.x + v1[1].x * cs2.y, v2[1].y * cs2.z + v1[1].y * cs2.w);
         store2(vc + base, v1[2].x, v1[2].y);
@@ -600,8 +617,9 @@ __global__ void __launch_bounds__(ROPW_THREADS, 4)
 }
 
 cudaError_t launch_rope_kv(float* qkv, const GemmOut& proj, void* kcache, void* vcache, const float* table,
-                           const RowTables& rt, const Dims& dm, int m_max, int* status, Chain* chain, cudaStream_t st) {
+                           const RowTables& rt, const Dims& dm, int m_max, int* status, Chain* chain, const KvPages* pages, cudaStream_t st) {
   const int n_items = dm.H * (dm.hd / 4);
+  const KvPages pg = pages ? *pages : KvPages{};
   dim3 grid(m_max, (n_items + ROPE_THREADS - 1) / ROPE_THREADS);
   if (m_max > WIDE_ROWS_MIN && ROPW_COLS % dm.hd == 0 && (ROPW_COLS / dm.hd) * (dm.hd / 4) <= ROPW_THREADS) {
     // several row tiles: four CTAs per SM (36 KB of stages each) walk the rows
@@ -610,13 +628,13 @@ cudaError_t launch_rope_kv(float* qkv, const GemmOut& proj, void* kcache, void* 
     const int gy = std::max(1, 4 * wide_sm_count() / (int)gw.x);   // no CTA beyond one wave
     gw.y = gy < m_max ? gy : m_max;
     const ChainSync cs = chain ? chain->link(gw.x * gw.y, true) : ChainSync{nullptr, 0u, nullptr, nullptr, nullptr};
-    launch_pdl(rope_kv_wide_kernel, gw, ROPW_THREADS, 0, st, qkv, proj, (__nv_bfloat16*)kcache, (__nv_bfloat16*)vcache,
-               reinterpret_cast<const float2*>(table), rt, dm, status, cs);
+    launch_pdl(pages ? rope_kv_wide_kernel<true> : rope_kv_wide_kernel<false>, gw, ROPW_THREADS, 0, st, qkv, proj, (__nv_bfloat16*)kcache,
+               (__nv_bfloat16*)vcache, reinterpret_cast<const float2*>(table), rt, dm, status, cs, pg);
     return cudaGetLastError();
   }
   const ChainSync cs = chain ? chain->link(grid.x * grid.y, true) : ChainSync{nullptr, 0u, nullptr, nullptr, nullptr};
-  launch_pdl(rope_kv_kernel, grid, ROPE_THREADS, 0, st, qkv, proj, (__nv_bfloat16*)kcache, (__nv_bfloat16*)vcache,
-             reinterpret_cast<const float2*>(table), rt, dm, status, cs);
+  launch_pdl(pages ? rope_kv_kernel<true> : rope_kv_kernel<false>, grid, ROPE_THREADS, 0, st, qkv, proj, (__nv_bfloat16*)kcache, (__nv_bfloat16*)vcache,
+             reinterpret_cast<const float2*>(table), rt, dm, status, cs, pg);
   return cudaGetLastError();
 }
 
@@ -1098,6 +1116,44 @@ cudaError_t launch_build_rows_ar(const int32_t* root, const int32_t* ctx, int32_
                                  int* status, cudaStream_t st) {
   launch_pdl(build_rows_ar_kernel, 1, B > 128 ? 256 : 128, 0, st, root, ctx, row_tok, row_seq, row_pos, row_slot, row_ncache,
                                                         row_local, row_out_index, seq_off, m_total, dm, B, status);
+  return cudaGetLastError();
+}
+
+__global__ void page_growth_kernel(const int32_t* __restrict__ seq_off, const int32_t* __restrict__ row_pos, const int32_t* __restrict__ seqs,
+                                   const int32_t* __restrict__ lens, int max_seqs, int B, int32_t* n_new, int32_t* status) {
+  pdl_enter();
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b >= B) return;
+  const int m = seq_off[b + 1] - seq_off[b], s = seqs ? seqs[b] : b;
+  n_new[b] = m;
+  if (m > 0 && ((unsigned)s >= (unsigned)max_seqs || lens[s] != row_pos[seq_off[b]])) atomicOr(status, DEV_ERR_INDEX_RANGE);
+}
+
+cudaError_t launch_page_growth(const int32_t* seq_off, const int32_t* row_pos, const int32_t* seqs, const int32_t* lens, int max_seqs, int B, int32_t* n_new,
+                               int32_t* status, cudaStream_t st) {
+  launch_pdl(page_growth_kernel, (B + 127) / 128, 128, 0, st, seq_off, row_pos, seqs, lens, max_seqs, B, n_new, status);
+  return cudaGetLastError();
+}
+
+// The token that follows a node of the accepted path is the LLM's own choice there.
+__global__ void emitted_rows_kernel(EmittedRows e, int BW, int32_t* row, int32_t* tok) {
+  pdl_enter();
+  const int idx = blockIdx.x * blockDim.x + threadIdx.x;
+  if (idx >= e.B * (e.L + 1)) return;
+  const int b = idx / (e.L + 1), j = idx - b * (e.L + 1);
+  int r = -1, t = -1;
+  if (e.tokens) {
+    if (j == 0) { r = b; t = e.tokens[b]; }
+  } else if (j <= e.n_accept[b]) {
+    const int i = e.best[b], n = (unsigned)i < (unsigned)BW ? e.unpack[((size_t)b * BW + i) * (e.L + 1) + j] : -1;
+    if ((unsigned)n < (unsigned)e.NMAX) { r = e.seq_off[b] + n; t = e.argmax[(size_t)b * e.NMAX + n]; }
+  }
+  row[idx] = r;
+  tok[idx] = t;
+}
+
+cudaError_t launch_emitted_rows(const EmittedRows& e, int BW, int32_t* row, int32_t* tok, cudaStream_t st) {
+  launch_pdl(emitted_rows_kernel, (e.B * (e.L + 1) + 127) / 128, 128, 0, st, e, BW, row, tok);
   return cudaGetLastError();
 }
 

@@ -119,6 +119,29 @@ bool aligned16(const void* p, long long stride, int es) { return ((uintptr_t)p &
 
 }  // namespace
 
+namespace rd {
+
+const PageView& pages_view(const rd_pages* h) { return h->pv; }
+int pages_device(const rd_pages* h) { return h->device; }
+
+cudaError_t pages_extend_for(rd_pages* h, const int32_t* seqs, const int32_t* n_new, int n, int* launches, cudaStream_t st) {
+  int mine = 0;
+  const cudaError_t e = launch_pages_extend(h->pv, seqs, n_new, n, h->scratch, &mine, st);
+  h->launches += mine;
+  *launches += mine;
+  return e;
+}
+
+// The kernel for the rows at hand: single tokens; many rows on the tensor cores; many rows of the fp32 configuration.
+cudaError_t pages_attention_for(rd_pages* h, const PageRows& rows, const PageAttention& a, cudaStream_t st) {
+  h->launches++;
+  if (rows.max_rows == 1) return launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, st);
+  if (h->pv.es == 2) return launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, h->grid, st);
+  return launch_pages_attention_plain(h->pv, h->dtype, rows, a, st);
+}
+
+}  // namespace rd
+
 extern "C" {
 
 size_t redrafter_pages_workspace_bytes(const rd_page_cache* cache) {
@@ -276,10 +299,7 @@ int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, c
   a.q = q; a.out = out; a.lse = lse; a.q_stride = q_stride; a.out_stride = out_stride; a.heads = n_heads; a.layer = layer;
   a.window = window; a.sinks = window ? sinks : 0;
   a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)h->pv.hd);
-  if (rows.max_rows == 1) PCK(launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, (cudaStream_t)stream));
-  else if (h->pv.es == 2) PCK(launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, h->grid, (cudaStream_t)stream));
-  else PCK(launch_pages_attention_plain(h->pv, h->dtype, rows, a, (cudaStream_t)stream));
-  h->launches++;
+  PCK(pages_attention_for(h, rows, a, (cudaStream_t)stream));
   return RD_OK;
 }
 

@@ -107,8 +107,26 @@ cudaError_t launch_embed_rope(int dtype, const void* emb, const int32_t* tok, co
                               int hd, float theta, const int32_t* m_total, int m_max, int* status, cudaStream_t st);
 cudaError_t launch_rmsnorm(int dtype, float* x, const GemmOut* proj, const void* gain, void* out_t, float* out_f32, int d,
                            float eps, const int32_t* m_total, int m_max, Chain* chain, cudaStream_t st);
+// Pages that take K and V in place of the contiguous cache, and the bf16 rows of the rotated Q for the attention that reads them.
+struct KvPages {
+  const int32_t* table;   // [max_seqs][max_pages]
+  const int32_t* seqs;    // table row of each of the batch's sequences, or nullptr: its index
+  __nv_bfloat16* q;       // [M][d]
+  int max_seqs, max_pages, n_pages, ps_log2;
+};
 cudaError_t launch_rope_kv(float* qkv, const GemmOut& proj, void* kcache, void* vcache, const float* table,
-                           const RowTables& rt, const Dims& dm, int m_max, int* status, Chain* chain, cudaStream_t st);
+                           const RowTables& rt, const Dims& dm, int m_max, int* status, Chain* chain, const KvPages* pages, cudaStream_t st);
+// Rows of every sequence in the pass (from seq_off), for the pages to grow by; reports sequences whose pages do not hold their
+// context (row_pos of their first row).
+cudaError_t launch_page_growth(const int32_t* seq_off, const int32_t* row_pos, const int32_t* seqs, const int32_t* lens, int max_seqs, int B, int32_t* n_new,
+                               int32_t* status, cudaStream_t st);
+// Row of the logits and token of everything that the last call emitted: [B][L + 1], -1 where nothing was.
+struct EmittedRows {
+  int B, L, NMAX;
+  const int32_t* tokens;     // one token per sequence, its row of the logits the sequence's index; or nullptr: the last step's
+  const int32_t *n_accept, *best, *unpack, *seq_off, *argmax;
+};
+cudaError_t launch_emitted_rows(const EmittedRows& e, int BW, int32_t* row, int32_t* tok, cudaStream_t st);
 cudaError_t launch_attention(int dtype, const float* qkv, const void* kcache, const void* vcache, void* out_t,
                              const RowTables& rt, const Dims& dm, int m_max, Chain* chain, cudaStream_t st);
 // Tensor-core attention (bf16): KV tiles staged through shared memory, split over the keys.
