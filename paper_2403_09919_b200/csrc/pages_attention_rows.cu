@@ -424,6 +424,7 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
           }
           // (the next chunk's K is waited for here: the MMA warp has no time to spare)
           if (c + 1 < it.n_chunks && !(ok = wait_warp(bar(K_FULL + (s ^ 1)), ((x + 1) >> 1) & 1))) break;
+          __syncwarp();   // (all lanes' zeros and looks before the one arrival)
           if (lane == 0) mbar_arrive(bar(V_OK + s));
         }
         g += it.n_chunks;
