@@ -703,7 +703,7 @@ int forward_layers(rd_handle* h, const uint32_t* mask, int m_max, int n_seq, int
       if (paged) {   // the normalised rows have been read: their place takes the rotated Q
         const PageView& pv = pages_view(h->pages);
         const size_t plane = (size_t)pv.n_pages * pv.H * pv.ps * pv.hd * pv.es;
-        kp = KvPages{pv.table, h->page_seqs, (__nv_bfloat16*)w.a_t, pv.max_seqs, pv.max_pages, pv.n_pages, pv.ps_log2};
+        kp = KvPages{pv.table, h->page_seqs, pv.refs, (__nv_bfloat16*)w.a_t, pv.max_seqs, pv.max_pages, pv.n_pages, pv.ps_log2};
         kc = (char*)pv.pool + (size_t)(2 * l) * plane; vc = (char*)kc + plane;
       }
       CKP(h, PROF_ROPE, launch_rope_kv(w.qkv, g_qkv, kc, vc, w.rope_tab, rt, dm, m_max, w.status, ch, paged ? &kp : nullptr, st));
@@ -1284,7 +1284,7 @@ int redrafter_last_logprobs(rd_handle* h, void* stream, int32_t top, float tempe
   const Dims& dm = h->dm;
   Workspace& w = h->ws;
   if (top < 0 || top > LOGPROB_MAX_TOP || top > dm.V) return fail(h, RD_ERR_SHAPE, "top %d (at most %d)", top, LOGPROB_MAX_TOP);
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) return fail(h, RD_ERR_INVALID_ARG, "temperature %g", (double)temperature);
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.5f / temperature)) return fail(h, RD_ERR_INVALID_ARG, "temperature %g", (double)temperature);
   if (top && (!top_ids || !top_logprobs)) return fail(h, RD_ERR_INVALID_ARG, "top_ids or top_logprobs is null");
   cudaStream_t st = (cudaStream_t)stream;
   const int B = h->batch;

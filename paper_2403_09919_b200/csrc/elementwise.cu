@@ -398,12 +398,13 @@ __device__ __forceinline__ void store2(__nv_bfloat16* p, float a, float b) {
 // the other: an argument and a test more cost an autoregressive step of the 7B shape 0.3 %).
 struct NoPages {};
 template <typename PG> inline constexpr bool paged = !std::is_same_v<PG, NoPages>;
-// Element of the layer's plane at which a row's head begins in its page, -1: nowhere.
+// Element of the layer's plane at which a row's head begins in its page, -1: nowhere (a page that another sequence names, too, is
+// not written: room for the row was not found).
 __device__ __forceinline__ long long page_row(const Dims& dm, const KvPages& pg, int b, int h, int slot) {
   const int s = pg.seqs ? pg.seqs[b] : b;
   if ((unsigned)s >= (unsigned)pg.max_seqs || slot < 0 || (slot >> pg.ps_log2) >= pg.max_pages) return -1ll;
   const int page = pg.table[(size_t)s * pg.max_pages + (slot >> pg.ps_log2)];
-  if ((unsigned)page >= (unsigned)pg.n_pages) return -1ll;
+  if ((unsigned)page >= (unsigned)pg.n_pages || pg.refs[page] != 1) return -1ll;
   return ((((long long)page * dm.H + h) << pg.ps_log2) + (slot & ((1 << pg.ps_log2) - 1))) * dm.hd;
 }
 // The rotated Q: in place for the attention kernels of the contiguous cache, as bf16 rows for those that read pages.

@@ -111,6 +111,7 @@ cudaError_t launch_rmsnorm(int dtype, float* x, const GemmOut* proj, const void*
 struct KvPages {
   const int32_t* table;   // [max_seqs][max_pages]
   const int32_t* seqs;    // table row of each of the batch's sequences, or nullptr: its index
+  const int32_t* refs;    // [n_pages]
   __nv_bfloat16* q;       // [M][d]
   int max_seqs, max_pages, n_pages, ps_log2;
 };

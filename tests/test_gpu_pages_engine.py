@@ -271,3 +271,27 @@ def test_log_probabilities_of_what_a_call_emitted():
         ar.eng.last_logprobs(top=65)
     with pytest.raises(binding.RdError):
         ar.eng.last_logprobs(temperature=0.0)
+
+
+def test_a_step_without_room_leaves_shared_pages_alone():
+    """Two sequences share a partly filled page and no page is free: the one that would have to copy it first is not written."""
+    r = Rig(cfg=CFG)
+    cache = pages_for(CFG, 16, n_pages=2, max_seqs=2, max_pages=4)
+    prompt = np.random.default_rng(5).integers(0, CFG["vocab"], size=20)
+    r.eng.use_pages(cache, dev(np.array([0, 1, 1, 1])))
+    r.eng.prefill([prompt])
+    cache.fork(dev(np.array([0])), dev(np.array([1])))
+    cache.compact(dev(np.array([2])), dev(np.array([0])), seqs=dev(np.array([1])))      # 18 of the 20 tokens
+    r.eng.poll()
+    cache.poll()
+    assert cache.lens.tolist() == [20, 18] and cache.refs.tolist() == [2, 2]
+    before = cache.pool.clone()
+    r.eng.use_pages(cache, dev(np.array([1, 0, 0, 0])))
+    r.eng.set_state(dev(np.array([18])), dev(np.array([7])), None, batch=1, ctx_bound=18)
+    r.eng.ar_step()
+    with pytest.raises(binding.RdError):
+        cache.poll()
+    with pytest.raises(binding.RdError):
+        r.eng.poll()
+    assert torch.equal(cache.pool.view(torch.int16), before.view(torch.int16))
+    assert cache.lens.tolist() == [20, 18]
