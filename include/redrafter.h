@@ -341,7 +341,7 @@ RD_API int redrafter_route_counts(const rd_handle* h, int64_t* out, int32_t n);
  * Pages are given out lowest index first, in the order of a call's sequences: what a call leaves does not depend on timing.
  *
  * The calls on one handle are issued in stream order on one stream at a time (their scratch is the handle's workspace; that
- * goes for graphs that captured them, too).  All of them may be captured.  A list of sequences `seqs` is a device array of
+ * goes for graphs that captured them, too).  All but poll may be captured.  A list of sequences `seqs` is a device array of
  * n rows of the table, or NULL: 0 .. n-1.  What a kernel finds out of range -- a sequence outside the table, a length, a
  * page, a row, a sequence named twice by a call that changes it -- it leaves out, and the next redrafter_pages_poll
  * reports it.  Errors of every call: INVALID_ARG, SHAPE, CUDA, STATE (another device than the handle's is current). */
@@ -350,7 +350,8 @@ typedef struct {
   int32_t n_layers, n_kv_heads, head_dim;     /* head_dim 64 or 128 */
   int32_t dtype;                              /* RD_DTYPE_* of the pool, and of the rows written to it and read against it */
   int32_t page_size;                          /* tokens: 16, 32, 64 or 128 */
-  int32_t n_pages, max_seqs, max_seq_pages;   /* n_layers * 2 * n_pages * n_kv_heads * page_size < 2^31 */
+  int32_t n_pages, max_seqs, max_seq_pages;   /* n_layers * 2 * n_pages * n_kv_heads * page_size, max_seqs * max_seq_pages and
+                                                 max_seq_pages * page_size * max(n_kv_heads, 2) < 2^31 */
   int32_t reserved;
   void* pool;
   int32_t* page_table;
@@ -417,7 +418,8 @@ RD_API int redrafter_pages_write(rd_pages* h, int32_t layer, const int32_t* seqs
  * q, out: [n_rows][n_heads][head_dim] of the cache's dtype, rows q_stride and out_stride elements apart and on 16-byte
  * boundaries, not overlapping; rows behind the last sequence's are left as they are.  lse: [n_rows][n_heads] fp32, the natural
  * logarithm of the softmax's denominator, or NULL.  scale 0: head_dim^-1/2.  max_rows: the most rows of any sequence, which
- * picks the kernel (the rows of a sequence that brings more are left as they are and reported); 0: n_rows.  A row without keys (an empty sequence,
+ * picks the kernel (the rows of a sequence that brings more are left as they are and reported); 0: n_rows.  A row that would see a page which the table does not name (trimmed too
+ * early, say) is reported and not defined.  At most 1024 query heads to a key and value head.  A row without keys (an empty sequence,
  * or all its scores -inf) gives zeros and -inf.  Keys that a row does not see do not reach it, whatever they hold.  Sums and the
  * softmax's statistics are in fp32; bf16: the weights that multiply V are rounded to bf16. */
 RD_API int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, const int32_t* row_off, int32_t n, int32_t n_rows, int32_t max_rows,

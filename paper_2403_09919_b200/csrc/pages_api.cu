@@ -16,6 +16,8 @@ namespace {
 struct alignas(64) MapBox {   // opaque storage of one CUtensorMap
   unsigned char bytes[128];
 };
+constexpr int MAX_ROWS = 1 << 30;     // rows of a call, and what a window is cut to (a sequence has fewer tokens): positions less a window fit 32 bits
+constexpr int MAX_GROUP = 1024;        // query heads of a key and value head
 constexpr int TOKEN_MAX_GRID = 160;   // upper bound of the SM count that the parts are sized for
 }  // namespace
 
@@ -74,12 +76,15 @@ bool view_of(const rd_page_cache* c, PageView* pv) {
   return true;
 }
 
-// head_dim 64 or 128, pages of 16 to 128 tokens, rows of one head and layer countable in 31 bits.
+// head_dim 64 or 128, pages of 16 to 128 tokens; the pool's rows, the table's entries and a sequence's tokens times its heads
+// (two at least, so that a position plus a tile fits, too) countable in 31 bits: what the kernels count in 32 bits then fits.
 bool view_shape_ok(const PageView& pv) {
   if (pv.hd != 64 && pv.hd != 128) return false;
   if (pv.ps < 16 || pv.ps > 128 || (1 << pv.ps_log2) != pv.ps) return false;
   if ((double)pv.n_layers * 2 * pv.n_pages * pv.H * pv.ps >= 2147483648.0) return false;   // rows of the pool
   if ((double)pv.n_layers * 2 * pv.H * pv.hd >= 2147483648.0) return false;
+  if ((double)pv.max_seqs * pv.max_pages >= 2147483648.0) return false;
+  if ((double)pv.max_pages * pv.ps * (pv.H > 2 ? pv.H : 2) >= 2147483648.0) return false;
   return true;
 }
 
@@ -96,16 +101,16 @@ int enter(rd_pages* h, int n) {
   return RD_OK;
 }
 // ... and those that take a list of sequences of the table.
-int enter_list(rd_pages* h, const int32_t* seqs, int n) {
+int enter_list(rd_pages* h, int n) {
   if (int rc = enter(h, n)) return rc;
   if (n > h->pv.max_seqs) return fail(h, RD_ERR_INVALID_ARG, "%d sequences, the table has %d", n, h->pv.max_seqs);
-  (void)seqs;
   return RD_OK;
 }
 
 int rows_ok(rd_pages* h, int layer, const int32_t* row_off, int n, int n_rows) {
   if (layer < 0 || layer >= h->pv.n_layers) return fail(h, RD_ERR_INVALID_ARG, "layer %d of %d", layer, h->pv.n_layers);
-  if (n_rows < 0 || (!row_off && n_rows != n)) return fail(h, RD_ERR_INVALID_ARG, "%d rows for %d sequences of one row each", n_rows, n);
+  if (n_rows < 0 || n_rows > MAX_ROWS) return fail(h, RD_ERR_INVALID_ARG, "%d rows", n_rows);
+  if (!row_off && n_rows != n) return fail(h, RD_ERR_INVALID_ARG, "%d rows for %d sequences of one row each", n_rows, n);
   return RD_OK;
 }
 
@@ -133,11 +138,12 @@ cudaError_t pages_extend_for(rd_pages* h, const int32_t* seqs, const int32_t* n_
 }
 
 // The kernel for the rows at hand: single tokens; many rows on the tensor cores; many rows of the fp32 configuration.
-cudaError_t pages_attention_for(rd_pages* h, const PageRows& rows, const PageAttention& a, cudaStream_t st) {
+cudaError_t pages_attention_for(rd_pages* h, const PageRows& rows, PageAttention a, cudaStream_t st) {
   h->launches++;
+  a.window = a.window < MAX_ROWS ? a.window : MAX_ROWS;
   if (rows.max_rows == 1) return launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, st);
   if (h->pv.es == 2) return launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, h->grid, st);
-  return launch_pages_attention_plain(h->pv, h->dtype, rows, a, st);
+  return launch_pages_attention_fp32(h->pv, rows, a, st);
 }
 
 }  // namespace rd
@@ -162,7 +168,7 @@ int redrafter_pages_init(const rd_page_cache* cache, void* workspace, size_t ws_
   PageView pv;
   if (!view_of(cache, &pv)) return init_fail(RD_ERR_INVALID_ARG, "struct_bytes, dtype or a size is out of range");
   if (!pv.pool || !pv.table || !pv.lens || !pv.refs || !pv.free_bits) return init_fail(RD_ERR_INVALID_ARG, "null buffer");
-  if (!view_shape_ok(pv)) return init_fail(RD_ERR_SHAPE, "head_dim %d (64 or 128), page_size %d (16, 32, 64 or 128) or a pool of 2^31 rows", pv.hd, pv.ps);
+  if (!view_shape_ok(pv)) return init_fail(RD_ERR_SHAPE, "head_dim %d (64 or 128), page_size %d (16, 32, 64 or 128), or 2^31 rows of the pool, entries of the table or tokens times heads of a sequence", pv.hd, pv.ps);
   if (((uintptr_t)pv.pool | (uintptr_t)workspace) & 255) return init_fail(RD_ERR_INVALID_ARG, "pool and workspace have to be 256-byte aligned");
   if (ws_bytes < page_workspace(pv)) return init_fail(RD_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", ws_bytes, page_workspace(pv));
   int dev = 0;
@@ -218,7 +224,7 @@ int redrafter_pages_reset(rd_pages* h, void* stream) {
 }
 
 int redrafter_pages_extend(rd_pages* h, const int32_t* seqs, const int32_t* n_new, int32_t n, void* stream) {
-  if (int rc = enter_list(h, seqs, n)) return rc;
+  if (int rc = enter_list(h, n)) return rc;
   if (!n_new) return fail(h, RD_ERR_INVALID_ARG, "n_new is null");
   if (n == 0) return RD_OK;
   int launches = 0;
@@ -228,7 +234,7 @@ int redrafter_pages_extend(rd_pages* h, const int32_t* seqs, const int32_t* n_ne
 }
 
 int redrafter_pages_fork(rd_pages* h, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
-  if (int rc = enter_list(h, dst, n)) return rc;
+  if (int rc = enter_list(h, n)) return rc;
   if (!src || !dst) return fail(h, RD_ERR_INVALID_ARG, "null list");
   if (n == 0) return RD_OK;
   PCK(launch_pages_fork(h->pv, src, dst, n, (cudaStream_t)stream));
@@ -238,7 +244,7 @@ int redrafter_pages_fork(rd_pages* h, const int32_t* src, const int32_t* dst, in
 
 int redrafter_pages_compact(rd_pages* h, const int32_t* seqs, const int32_t* n_rows, const int32_t* n_keep, const int32_t* rows,
                             int32_t row_stride, int32_t n, void* stream) {
-  if (int rc = enter_list(h, seqs, n)) return rc;
+  if (int rc = enter_list(h, n)) return rc;
   if (!n_rows || !n_keep) return fail(h, RD_ERR_INVALID_ARG, "null list");
   if (rows && row_stride <= 0) return fail(h, RD_ERR_INVALID_ARG, "row_stride %d", row_stride);
   if (n == 0) return RD_OK;
@@ -249,7 +255,7 @@ int redrafter_pages_compact(rd_pages* h, const int32_t* seqs, const int32_t* n_r
 }
 
 int redrafter_pages_trim(rd_pages* h, const int32_t* seqs, int32_t window, int32_t sinks, int32_t n, void* stream) {
-  if (int rc = enter_list(h, seqs, n)) return rc;
+  if (int rc = enter_list(h, n)) return rc;
   if (window < 1 || sinks < 0) return fail(h, RD_ERR_INVALID_ARG, "window %d, sinks %d", window, sinks);
   if (n == 0) return RD_OK;
   PCK(launch_pages_trim(h->pv, seqs, window, sinks, n, (cudaStream_t)stream));
@@ -258,7 +264,7 @@ int redrafter_pages_trim(rd_pages* h, const int32_t* seqs, int32_t window, int32
 }
 
 int redrafter_pages_free(rd_pages* h, const int32_t* seqs, int32_t n, void* stream) {
-  if (int rc = enter_list(h, seqs, n)) return rc;
+  if (int rc = enter_list(h, n)) return rc;
   if (n == 0) return RD_OK;
   PCK(launch_pages_free(h->pv, seqs, n, (cudaStream_t)stream));
   h->launches++;
@@ -267,7 +273,7 @@ int redrafter_pages_free(rd_pages* h, const int32_t* seqs, int32_t n, void* stre
 
 int redrafter_pages_write(rd_pages* h, int32_t layer, const int32_t* seqs, const int32_t* row_off, int32_t n, int32_t n_rows, const void* k,
                           int64_t k_stride, const void* v, int64_t v_stride, void* stream) {
-  if (int rc = enter_list(h, seqs, n)) return rc;
+  if (int rc = enter_list(h, n)) return rc;
   if (int rc = rows_ok(h, layer, row_off, n, n_rows)) return rc;
   if (n == 0 || n_rows == 0) return RD_OK;
   if (!k || !v) return fail(h, RD_ERR_INVALID_ARG, "k or v is null");
@@ -285,7 +291,7 @@ int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, c
                               int32_t window, int32_t sinks, void* stream) {
   if (int rc = enter(h, n)) return rc;
   if (int rc = rows_ok(h, layer, row_off, n, n_rows)) return rc;
-  if (n_heads <= 0 || n_heads % h->pv.H) return fail(h, RD_ERR_SHAPE, "%d query heads on %d key and value heads", n_heads, h->pv.H);
+  if (n_heads <= 0 || n_heads % h->pv.H || n_heads / h->pv.H > MAX_GROUP) return fail(h, RD_ERR_SHAPE, "%d query heads on %d key and value heads", n_heads, h->pv.H);
   if (window < 0 || sinks < 0) return fail(h, RD_ERR_INVALID_ARG, "window %d, sinks %d", window, sinks);
   if (!std::isfinite(scale) || scale < 0.f) return fail(h, RD_ERR_INVALID_ARG, "scale %g", (double)scale);
   if (max_rows < 0) return fail(h, RD_ERR_INVALID_ARG, "max_rows %d", max_rows);
@@ -311,8 +317,6 @@ int redrafter_pages_poll(rd_pages* h, void* stream) {
   PCK(cudaStreamSynchronize(st));
   if (v == 0) return RD_OK;
   PCK(cudaMemsetAsync(h->pv.status, 0, sizeof(int32_t), st));
-  if (v & DEV_ERR_TIMEOUT)   // a launch that gave up may have left counters behind
-    PCK(cudaMemsetAsync(h->parts, 0, pages_token_part_bytes(h->pv, TOKEN_MAX_GRID), st));
   if (v & DEV_ERR_TIMEOUT) return fail(h, RD_ERR_TIMEOUT, "device status 0x%x: a bounded wait gave up", v);
   if (v & DEV_ERR_CAPACITY) return fail(h, RD_ERR_CAPACITY, "device status 0x%x: too few free pages, a call that extends changed nothing", v);
   return fail(h, RD_ERR_INVALID_ARG, "device status 0x%x: a sequence, length, row or page out of range was skipped", v);
@@ -324,7 +328,7 @@ int redrafter_token_logprobs(const rd_logprobs* args, void* stream) {
   if (p.dtype != RD_DTYPE_FP32 && p.dtype != RD_DTYPE_BF16) return logprob_fail(RD_ERR_INVALID_ARG, "dtype %d", p.dtype);
   if (p.rows < 0 || p.n_logit_rows < 0 || p.vocab <= 0 || p.vocab > (1 << 30)) return logprob_fail(RD_ERR_INVALID_ARG, "%d rows of %d, vocabulary %d", p.rows, p.n_logit_rows, p.vocab);
   if (p.top < 0 || p.top > LOGPROB_MAX_TOP || p.top > p.vocab) return logprob_fail(RD_ERR_SHAPE, "top %d of %d (at most %d)", p.top, p.vocab, LOGPROB_MAX_TOP);
-  if (!(p.temperature > 0.f) || !std::isfinite(p.temperature) || !std::isfinite(1.f / p.temperature)) return logprob_fail(RD_ERR_INVALID_ARG, "temperature %g", (double)p.temperature);
+  if (!(p.temperature > 0.f) || !std::isfinite(p.temperature) || !std::isfinite(1.5f / p.temperature)) return logprob_fail(RD_ERR_INVALID_ARG, "temperature %g", (double)p.temperature);
   if (p.rows == 0) return RD_OK;
   if (!p.logits || (p.logprob && !p.tokens) || (p.top && (!p.top_ids || !p.top_logprobs))) return logprob_fail(RD_ERR_INVALID_ARG, "null buffer");
   if (!p.row_index && p.rows > p.n_logit_rows) return logprob_fail(RD_ERR_INVALID_ARG, "%d rows of %d", p.rows, p.n_logit_rows);

@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
       const int st = n % TK_STAGES;
       const int k0 = first_key(item.s, item.chunk + x) + wkey;
       ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * st, (n / TK_STAGES) & 1, abort_flag, pv.status));
-      if (!ok) break;
+      if (!ok) { n += todo - x; break; }   // (the warps still meet below, and the parts' counters come back to zero)
       const uint32_t sk = wbase + (uint32_t)(st * STAGE), sv = sk + STAGE / 2;
       // which of the 16 keys the row sees
       uint32_t seen = 0xffffu;
@@ -480,7 +480,6 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
       __syncwarp();
       if (lane == 0) mbar_arrive(bars + 8u * (TK_STAGES + st));
     }
-    if (!ok) return;
     // ---- join the warps through shared memory
     consumers_sync();   // the join before has been read
 #pragma unroll
@@ -569,6 +568,12 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_f32_kernel(const To
         if (n >= TF_STAGES && !(ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * (TF_STAGES + st), ((n / TF_STAGES) & 1) ^ 1u, abort_flag, pv.status)))) break;
         const bool mine = u == x && b.wanted && b.page >= 0;
         const uint32_t count = __popc(__ballot_sync(0xffffffffu, mine));
+        if (u == x && b.wanted && b.page < 0) {   // (reported; zeros, as the copy of the other type fills in, not what the slot held before)
+          for (uint32_t e = 0; e < bytes; e += 16)
+            for (int kv = 0; kv < 2; ++kv) *reinterpret_cast<float4*>(gen + st * STAGE + kv * (STAGE / 2) + (size_t)box * bytes + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncwarp();
         if (lane == 0) mbar_expect_tx(bars + 8u * st, count * 2 * bytes);
         __syncwarp();
         if (mine) {
@@ -609,7 +614,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_f32_kernel(const To
     for (int x = 0; x < todo; ++x, ++n) {
       const int st = n % TF_STAGES, k0 = first_key(item.s, item.chunk + x) + wkey, j = k0 + key;
       ok = __all_sync(0xffffffffu, mbar_wait(bars + 8u * st, (n / TF_STAGES) & 1, abort_flag, pv.status));
-      if (!ok) break;
+      if (!ok) { n += todo - x; break; }   // (the warps still meet below, and the parts' counters come back to zero)
       const bool seen = j < item.s.len && (j >= item.s.start || j < item.s.sink_end);
       const uint32_t any = __ballot_sync(0xffffffffu, seen);
       if (any) {
@@ -661,7 +666,6 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_f32_kernel(const To
       __syncwarp();
       if (lane == 0) mbar_arrive(bars + 8u * (TF_STAGES + st));
     }
-    if (!ok) return;
     // ---- join the warps
 #pragma unroll
     for (int r = 0; r < R; ++r) {

@@ -297,3 +297,45 @@ def test_refusals():
         cache.write(1, keys[0][:1], values[0][:1])
     assert cache.launch_count() == n
     cache.poll()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [[1, 1, 1], [300, 40, 700]])
+def test_the_widest_window_is_no_window(dtype, rows):
+    """Positions before the first token less a window of 2^31 - 1 (a sequence of fewer tokens than rows) leave 32 bits."""
+    lens = [5, 40, 700]
+    cache, table, q, keys, values = build(lens, [min(m, n) for m, n in zip(rows, lens)], 4, 2, 128, 16, dtype)
+    q = torch.randn(sum(rows), 4, 128, device="cuda:0").to(DT[dtype])
+    kw = dict(row_off=dev(np.concatenate([[0], np.cumsum(rows)])), max_rows=max(rows)) if max(rows) > 1 else {}
+    want = cache.attention(0, q, **kw)
+    for window, sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 30, 7), (701, 0)):
+        assert torch.equal(cache.attention(0, q, window=window, sinks=sinks, **kw), want)
+    cache.poll()
+    compare(want[-rows[2]:], None, q[-rows[2]:], keys[2:], values[2:], lens[2:], rows[2:], 0, 0)
+
+
+def test_a_missing_page_of_the_fp32_configuration():
+    """A page that the table does not name, where a token looks: reported; what the copy's slot held before is not read."""
+    cache, table, q, keys, values = build([400, 400], [1, 1], 4, 2, 128, 16, "fp32")
+    want = cache.attention(0, q)
+    cache.poll()
+    cache.pool[0, :, torch.from_numpy(table[1, :25].copy()).to("cuda:0")] = 1e30      # (sequence 1, which the same CTAs may have read)
+    cache.page_table[0, 3] = -1
+    got = cache.attention(0, q)
+    with pytest.raises(binding.RdError) as e:
+        cache.poll()
+    assert e.value.code == 1
+    assert got[0].abs().max() < 100
+    cache.page_table[0, 3] = int(table[0, 3])
+    assert torch.equal(cache.attention(0, q)[0], want[0])
+    cache.poll()
+
+
+def test_refused_heads():
+    cache, table, q, keys, values = build([20], [1], 2, 1, 64, 16, "bf16")
+    for heads in (1025, 5000):
+        with pytest.raises(binding.RdError) as e:
+            cache.attention(0, torch.zeros(1, heads, 64, dtype=torch.bfloat16, device="cuda:0"))
+        assert e.value.code == 2
+    wide = torch.randn(1, 1024, 64, device="cuda:0").bfloat16()
+    compare(cache.attention(0, wide), None, wide, keys, values, [20], [1], 0, 0)

@@ -64,3 +64,19 @@ def test_there_is_no_cpu_path():
     i = torch.zeros(1, 1, dtype=torch.int32)
     with pytest.raises(RuntimeError):
         binding.PagedCache(torch.zeros(1, 2, 1, 1, 16, 64), i, i[0], i[0], i[0])
+
+
+def test_sizes_that_do_not_fit_what_the_kernels_count_in():
+    """Entries of the table, and a sequence's tokens times its heads (two at least), below 2^31."""
+    L = binding.lib()
+    for bad, good in ((dict(max_seqs=1 << 16, max_seq_pages=1 << 15), dict(max_seqs=(1 << 16) - 1, max_seq_pages=1 << 15, page_size=16)),
+                      (dict(max_seq_pages=1 << 23), dict(max_seq_pages=(1 << 23) - 1)),                          # 2^29 tokens of 4 heads
+                      (dict(n_kv_heads=1, max_seq_pages=1 << 24), dict(n_kv_heads=1, max_seq_pages=(1 << 24) - 1))):   # 2^30 tokens
+        assert L.redrafter_pages_workspace_bytes(C.byref(cache(**bad))) == 0, bad
+        assert L.redrafter_pages_workspace_bytes(C.byref(cache(**good))) > 0, good
+
+
+def test_a_temperature_whose_reciprocal_in_base_two_is_no_number():
+    L = binding.lib()
+    a = binding.RdLogprobs(struct_bytes=C.sizeof(binding.RdLogprobs), dtype=0, rows=1, n_logit_rows=1, vocab=8, temperature=3.2e-39, row_stride=8, logits=4096)
+    assert L.redrafter_token_logprobs(C.byref(a), None) == 1
