@@ -714,7 +714,9 @@ int forward_layers(rd_handle* h, const uint32_t* mask, int m_max, int n_seq, int
       a.q = w.a_t; a.out = w.attn_t; a.q_stride = a.out_stride = dm.d; a.heads = dm.H; a.layer = l;
       a.window = h->page_window; a.sinks = h->page_sinks; a.scale = 1.f / sqrtf((float)dm.hd);
       h->route[RD_ROUTE_ATT_PAGES]++;
-      CK(h, pages_attention_for(h->pages, PageRows{h->page_seqs, w.seq_off, n_seq, m_max, rows_per_seq_max}, a, st));
+      int launches = 0;
+      CKRT(h, pages_attention_for(h->pages, PageRows{h->page_seqs, w.seq_off, n_seq, m_max, rows_per_seq_max}, a, &launches, st));
+      h->launches += launches;
     } else {
       ProfScope ps(h, 1, 0.0, st);
       h->route[ap.kl ? RD_ROUTE_ATT_KEYS_ON_LANES : ap.t5 ? RD_ROUTE_ATT_ROWS128_TC5 : ap.wide ? RD_ROUTE_ATT_ROWS64

@@ -75,7 +75,9 @@ cudaError_t pages_token_prepare(const PageView& pv);
 cudaError_t launch_pages_token(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int grid, cudaStream_t st);
 // many rows per sequence, bf16
 cudaError_t pages_rows_prepare(int hd);
-cudaError_t launch_pages_rows(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, int sms, cudaStream_t st);
+size_t pages_rows_part_bytes(const PageView& pv, int grid);
+cudaError_t launch_pages_rows(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int sms, int* launches,
+                              cudaStream_t st);
 // many rows per sequence, fp32
 cudaError_t launch_pages_attention_fp32(const PageView& pv, const PageRows& rows, const PageAttention& a, cudaStream_t st);
 
@@ -83,6 +85,6 @@ cudaError_t launch_pages_attention_fp32(const PageView& pv, const PageRows& rows
 const PageView& pages_view(const rd_pages* h);
 int pages_device(const rd_pages* h);
 cudaError_t pages_extend_for(rd_pages* h, const int32_t* seqs, const int32_t* n_new, int n, int* launches, cudaStream_t st);
-cudaError_t pages_attention_for(rd_pages* h, const PageRows& rows, PageAttention a, cudaStream_t st);
+cudaError_t pages_attention_for(rd_pages* h, const PageRows& rows, PageAttention a, int* launches, cudaStream_t st);
 
 }  // namespace rd

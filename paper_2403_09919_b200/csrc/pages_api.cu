@@ -28,6 +28,7 @@ struct rd_pages {
   int dtype, device;
   int32_t* scratch;
   char* parts;      // joins of the attention kernel for single tokens
+  char* row_parts;  // ... of the one for many rows
   int grid;         // SMs
   int64_t launches;
   char err[256];
@@ -89,7 +90,7 @@ bool view_shape_ok(const PageView& pv) {
 }
 
 size_t scratch_bytes(const PageView& pv) { return (pages_scratch_ints(pv) * 4 + 255) / 256 * 256; }
-size_t page_workspace(const PageView& pv) { return 256 + scratch_bytes(pv) + pages_token_part_bytes(pv, TOKEN_MAX_GRID); }
+size_t page_workspace(const PageView& pv) { return 256 + scratch_bytes(pv) + pages_token_part_bytes(pv, TOKEN_MAX_GRID) + pages_rows_part_bytes(pv, TOKEN_MAX_GRID); }
 
 // What every call on a handle checks first.
 int enter(rd_pages* h, int n) {
@@ -138,12 +139,19 @@ cudaError_t pages_extend_for(rd_pages* h, const int32_t* seqs, const int32_t* n_
 }
 
 // The kernel for the rows at hand: single tokens; many rows on the tensor cores; many rows of the fp32 configuration.
-cudaError_t pages_attention_for(rd_pages* h, const PageRows& rows, PageAttention a, cudaStream_t st) {
-  h->launches++;
+cudaError_t pages_attention_for(rd_pages* h, const PageRows& rows, PageAttention a, int* launches, cudaStream_t st) {
+  int mine = 0;
   a.window = a.window < MAX_ROWS ? a.window : MAX_ROWS;
-  if (rows.max_rows == 1) return launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, st);
-  if (h->pv.es == 2) return launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, h->grid, st);
-  return launch_pages_attention_fp32(h->pv, rows, a, st);
+  cudaError_t e;
+  if (rows.max_rows > 1 && h->pv.es == 2) {
+    e = launch_pages_rows(h->map_rows.bytes, h->pv, rows, a, h->row_parts, h->grid, &mine, st);
+  } else {
+    e = rows.max_rows == 1 ? launch_pages_token(h->map_parts.bytes, h->pv, rows, a, h->parts, h->grid, st) : launch_pages_attention_fp32(h->pv, rows, a, st);
+    mine = 1;
+  }
+  h->launches += mine;
+  if (launches) *launches += mine;
+  return e;
 }
 
 }  // namespace rd
@@ -179,6 +187,7 @@ int redrafter_pages_init(const rd_page_cache* cache, void* workspace, size_t ws_
   h->pv.status = (int32_t*)workspace;
   h->scratch = (int32_t*)((char*)workspace + 256);
   h->parts = (char*)h->scratch + scratch_bytes(pv);
+  h->row_parts = h->parts + pages_token_part_bytes(pv, TOKEN_MAX_GRID);
   cudaError_t e = cudaDeviceGetAttribute(&h->grid, cudaDevAttrMultiProcessorCount, dev);
   if (h->grid > TOKEN_MAX_GRID) h->grid = TOKEN_MAX_GRID;
   if (e == cudaSuccess && pv.es == 2) {
@@ -305,7 +314,7 @@ int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, c
   a.q = q; a.out = out; a.lse = lse; a.q_stride = q_stride; a.out_stride = out_stride; a.heads = n_heads; a.layer = layer;
   a.window = window; a.sinks = window ? sinks : 0;
   a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)h->pv.hd);
-  PCK(pages_attention_for(h, rows, a, (cudaStream_t)stream));
+  PCK(pages_attention_for(h, rows, a, nullptr, (cudaStream_t)stream));
   return RD_OK;
 }
 

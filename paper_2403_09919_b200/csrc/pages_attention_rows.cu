@@ -16,6 +16,16 @@
 // Tensor memory: columns 0 and 128 S (and P) of A and B, 256 and 384 their O.
 // The CTAs stay (one per SM) and take one item after another, so that the next one's Q, K and V are on their way while the last
 // products and the output of one are finished.
+// Few items (up to half the SMs) leave SMs idle and take long over long contexts: their keys are then shared by up to 8 CTAs, at
+// least 4 chunks each, which leave unscaled outputs, maxima and sums (fp32) in the workspace, joined by rows_join_kernel.  Bf16, one
+// sequence, 32 query heads on 8, one CTA an item | shared: 256 rows of 8192 tokens 120 | 46.5 us, 500 rows 121 | 76; up to 16 CTAs
+// are slower again (64 rows of 8192 tokens 30.8 us with 8, 37.8 with 16: the join).
+// Few rows on grouped heads (rows x group up to 256) fill a tile with all the query heads of a key and value head: K and V are read
+// and multiplied once for all of them.  A head an item | packed: 16 sequences of 2000 tokens, 6 rows each 122 | 36 us; 64 of 500
+// tokens, 4 rows each 140 | 51; 17 rows of 8192 tokens 39.4 | 26.9; 60 rows of 300 tokens 15.1 | 18.5 (the one that loses: two
+// tiles after one another where idle SMs could take one each; the contexts' lengths stand on the device, and from about 1000 tokens
+// on it wins).
+// Launches that need neither take the forms without them (4096 rows: 2 us less than one kernel for all).
 // Roles: warp 0 finds the items and loads K and V by TMA, warp 1 MMA (the whole warp runs the loop, an elected lane issues), warps
 // 2 and 3 look through V, warps 4-7 softmax A, 8-11 softmax B.  Registers: 384 x 168 = 64,512 at launch; 4 warps go down to 120 and 8 up to 192
 // (128 x 120 + 256 x 192 = 64,512).  Every wait is bounded; on expiry the CTA reports and leaves.
@@ -24,8 +34,14 @@
 // overwritten by zeros, and chunks that only some rows see are looked through: where such a chunk holds NaN or infinities,
 // 0 x V would reach the others, and the CTA's rows are worked out one by one instead.
 //
-// Bounds: 2 x 1024 cycles of exponentials a chunk and pair of tiles (16 a cycle and SM) against 2048 of products.
+// Bounds: a chunk and pair of tiles takes some 3300 cycles where all of it is seen, against 2048 of products and 2 x 1024 of
+// exponentials (16 a cycle and SM); chunks that need masks take 1300 more, an item's set-up and output 5000.  What bounds it is each
+// tile's chain of scores, softmax and products, of which the other tile hides a part.  4096 rows of 32 heads, window 1024: 128 us
+// with the write of K and V (466 TFLOP/s of what the rows see; 512 items in four waves of 148).  Tried and slower: a warp issuing
+// for each tile (132 us), an eighth to a quarter of the exponentials as polynomials (130 to 134).
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "pages_attention.cuh"
 #include "pdl.cuh"
@@ -42,12 +58,20 @@ constexpr int RW_THREADS = 384;
 constexpr uint32_t RW_BLOCK = 128 * 128;   // bytes of 128 rows of 64 columns
 constexpr float RW_SLACK = 8.f;
 constexpr int RW_SLOTS = 4;                // published items
+constexpr int RW_MAX_SPLIT = 8, RW_MIN_CHUNKS = 4;   // CTAs that share an item's keys; chunks that each of them takes at least
+constexpr int RW_ROWS = 2 * RW_TILE;
 
 struct RowsParams {
   PageView pv;
   PageRows rows;
   PageAttention a;
+  int grid;        // CTAs of the launch
+  int pack;        // query heads that share a tile: 1, or all of a key and value head's (then an entry's rows are one item)
+  float* parts;    // [CTAs][rows_part_floats]: what they leave of an item that several work on
 };
+// A part: the unscaled output [HD / 4][RW_ROWS] of four dimensions each (a warp's store covers 512 bytes), then maximum (base 2) and
+// sum of every row.  A sum of NaN asks for the row to be worked out by itself.
+template <int HD> __host__ __device__ constexpr int rows_part_floats() { return RW_ROWS * (HD + 2); }
 
 __device__ __forceinline__ uint64_t desc_mnmajor_v(uint32_t addr) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(RW_BLOCK >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
@@ -67,29 +91,34 @@ __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 
 
 // What a CTA works on next, worked out by the producer warp and published two items ahead.
 struct RowsItem {
-  int head, row0, n_rows, pos0, seq;   // head -1: there is nothing left; pos0: position of the first row
+  int head, row0, n_rows, pos0, seq;   // head (of the heads / pack) -1: there is nothing left; n_rows: rows times pack; pos0: position of the first row
   // The keys as a list of boxes: 0 .. sink_boxes - 1 hold sinks, those from `first` on are box b + skew of the sequence, and the
   // places between them are left empty.
   int n_chunks, sink_boxes, skew, first;
   int start, end, sinks;      // keys that some row sees: [0, sinks) and [start, end)
   int to_a, from_b, to_b;     // chunks that a tile works on; A from the first
+  int c0, c1, part;           // SPLIT: chunks of this CTA; its part, -1: all of them
   int all_from, all_to_a, all_to_b, all_from_b;   // chunks that every row of a tile (A: all_from .. all_to_a) sees whole
   int unclean;                // V holds NaN or infinities that only some of the rows see
 
-  __device__ __forceinline__ int from(int tile) const { return tile ? from_b : 0; }
+  template <bool SPLIT> __device__ __forceinline__ int begin() const { return SPLIT ? c0 : 0; }
+  template <bool SPLIT> __device__ __forceinline__ int end_chunk() const { return SPLIT ? c1 : n_chunks; }
+  template <bool SPLIT> __device__ __forceinline__ int from(int tile) const { return tile ? from_b : begin<SPLIT>(); }
   __device__ __forceinline__ int to(int tile) const { return tile ? to_b : to_a; }
-  __device__ __forceinline__ bool active(int tile, int c) const { return c >= from(tile) && c < to(tile); }
-  __device__ __forceinline__ bool has(int tile) const { return to(tile) > from(tile); }
+  template <bool SPLIT> __device__ __forceinline__ bool active(int tile, int c) const { return c >= from<SPLIT>(tile) && c < to(tile); }
+  template <bool SPLIT> __device__ __forceinline__ bool has(int tile) const { return to(tile) > from<SPLIT>(tile); }
   // first key of box b; a place that is left empty: out of sight of everything
   __device__ __forceinline__ int base(int b, int box_log2) const {
     return b < sink_boxes ? b << box_log2 : b < first ? 0x7fffff00 : (b + skew) << box_log2;
   }
 };
 
-__device__ __forceinline__ void plan_rows(RowsItem& r, int window, int sinks, int box_log2) {
+// Row x of an item is token x / pack of its rows, query head x mod pack of those that share the tile.
+__device__ __forceinline__ void plan_rows(RowsItem& r, int window, int sinks, int box_log2, int pack) {
   const int box = 1 << box_log2, pc_log2 = 7 - box_log2, per_chunk = 1 << pc_log2;
   const bool two = r.n_rows > RW_TILE;
-  r.end = max(0, r.pos0 + r.n_rows);
+  const int last = (r.n_rows - 1) / pack, last_a = min(last, (RW_TILE - 1) / pack), first_b = RW_TILE / pack;   // tokens of the item
+  r.end = max(0, r.pos0 + last + 1);
   r.start = window > 0 ? max(0, r.pos0 - window + 1) : 0;
   r.sinks = min(sinks, r.start);
   const int first_box = r.start >> box_log2, end_box = (r.end + box - 1) >> box_log2;
@@ -100,10 +129,11 @@ __device__ __forceinline__ void plan_rows(RowsItem& r, int window, int sinks, in
   r.skew = end_box - (r.n_chunks << pc_log2);
   r.first = first_box - r.skew;
   // A stops behind its own last row's key, B begins (without sinks) where its first row's window does
-  const int end_a = max(0, min(r.pos0 + RW_TILE, r.end)), start_b = window > 0 ? max(0, r.pos0 + RW_TILE - window + 1) : 0;
+  const int end_a = max(0, r.pos0 + last_a + 1), start_b = window > 0 ? max(0, r.pos0 + first_b - window + 1) : 0;
   r.to_a = !two ? r.n_chunks : end_a > 0 ? min(r.n_chunks, (((end_a + box - 1) >> box_log2) - r.skew + per_chunk - 1) >> pc_log2) : 0;
   r.from_b = two && sinks == 0 && r.n_chunks > 0 ? max(0, (start_b >> box_log2) - r.skew) >> pc_log2 : 0;
   r.to_b = two ? r.n_chunks : 0;
+  r.c0 = 0; r.c1 = r.n_chunks; r.part = -1;
   // Chunk c of the window's part holds the keys k0 .. k0 + 127, k0 = (c * per_chunk + skew) * box.  Rows at positions p .. q see
   // all of it if k0 + 127 <= p and k0 > q - window.
   auto all_to = [&](int p) { return p < RW_KEYS - 1 ? 0 : (((p - (RW_KEYS - 1)) >> box_log2) - r.skew + per_chunk) >> pc_log2; };
@@ -111,11 +141,71 @@ __device__ __forceinline__ void plan_rows(RowsItem& r, int window, int sinks, in
     const int c0 = (r.first + per_chunk - 1) >> pc_log2;   // the first chunk without sinks and empty places
     return window > 0 && q >= window ? max(c0, (((q - window + box) >> box_log2) - r.skew + per_chunk - 1) >> pc_log2) : c0;
   };
-  r.all_from = all_from(r.pos0 + min(r.n_rows, RW_TILE) - 1);
+  r.all_from = all_from(r.pos0 + last_a);
   r.all_to_a = all_to(r.pos0);
-  r.all_from_b = all_from(r.pos0 + r.n_rows - 1);
-  r.all_to_b = all_to(r.pos0 + RW_TILE);
+  r.all_from_b = all_from(r.pos0 + last);
+  r.all_to_b = all_to(r.pos0 + first_b);
 }
+
+// Most CTAs that may share an item's keys: beyond 1 every CTA of the launch has one item at most.
+__device__ __forceinline__ int split_of(long long items, int grid) { return items > 0 ? (int)max(1ll, min((long long)RW_MAX_SPLIT, grid / items)) : 1; }
+// ... and those that do.
+__device__ __forceinline__ int parts_of(const RowsItem& r, int split) { return min(split, max(1, r.n_chunks / RW_MIN_CHUNKS)); }
+// What CTA w of the launch takes of an item that `split` CTAs may share: false for nothing.
+__device__ __forceinline__ bool cut_keys(RowsItem& r, int split, int w) {
+  const int n = parts_of(r, split), s = w % split;
+  if (s >= n) return false;
+  if (n > 1) {
+    r.part = w;
+    r.c0 = r.n_chunks * s / n; r.c1 = r.n_chunks * (s + 1) / n;
+    r.to_a = min(r.to_a, r.c1);
+    r.from_b = max(r.from_b, r.c0); r.to_b = min(r.to_b, r.c1);
+  }
+  return true;
+}
+
+// A lane's entry of a group of 32: its first row, rows, pairs of tiles, sequence and length.
+struct RowsEntries {
+  int first = 0, m = 0, pairs = 0, seq = -1, len = 0, group = -1;
+
+  __device__ __forceinline__ void look_up(const PageView& pv, const PageRows& rows, int pack, int i0) {
+    if (i0 == group) return;
+    group = i0; first = m = pairs = len = 0; seq = -1;
+    const int i = i0 + (int)(threadIdx.x & 31);
+    if (i >= rows.n) return;
+    seq = page_seq_of(pv, rows.seqs, i);
+    page_rows_of(rows, i, &first, &m);
+    if (seq >= 0) len = page_len_of(pv, seq);
+    pairs = m > rows.max_rows ? 0 : (int)(((long long)m * pack + RW_ROWS - 1) / RW_ROWS);
+  }
+  // The item of pair `slot` of all entries' (whole warp): false if there is none.
+  __device__ __forceinline__ bool find(const PageView& pv, const PageRows& rows, int pack, int slot, RowsItem& it) {
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int i0 = 0; i0 < rows.n; i0 += 32) {
+      look_up(pv, rows, pack, i0);
+      int incl = pairs;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      const int at = before + incl - pairs;
+      const uint32_t here = __ballot_sync(0xffffffffu, slot >= at && slot < at + pairs);
+      if (here) {
+        const int src = __ffs(here) - 1;
+        const int skip = (slot - __shfl_sync(0xffffffffu, at, src)) * RW_ROWS, rows_here = __shfl_sync(0xffffffffu, m, src);
+        it.row0 = __shfl_sync(0xffffffffu, first, src) + skip;
+        it.n_rows = min(RW_ROWS, (rows_here - skip) * pack);   // (pack > 1: one item, skip is 0)
+        it.pos0 = __shfl_sync(0xffffffffu, len, src) - rows_here + skip;
+        it.seq = __shfl_sync(0xffffffffu, seq, src);
+        return true;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    return false;
+  }
+};
 
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   uint64_t r;
@@ -145,7 +235,8 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool t
 constexpr int RW_STAGE_OUT = 32 * 128;     // bytes of a softmax warp's output on its way: 32 rows of 64 columns
 template <int HD> constexpr size_t rows_smem() { return 1024 + (size_t)(2 + 2 * RW_STAGES) * (HD / 64) * RW_BLOCK + 8 * RW_STAGE_OUT + 1024; }
 
-template <int HD>
+// PACK: p.pack > 1.
+template <int HD, bool SPLIT, bool PACK>
 __global__ void __launch_bounds__(RW_THREADS, 1)
     pages_rows_kernel(const __grid_constant__ CUtensorMap map, const RowsParams p) {
   extern __shared__ uint8_t smem_raw[];
@@ -184,9 +275,11 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  pdl_enter();
+  pdl_wait();
+  pdl_launch_dependents();   // (in this order: rows_join_kernel looks at the lists and lengths before its own wait)
 
-  const int window = p.a.window, sinks = p.a.sinks, group = p.a.heads / pv.H, box_log2 = min(pv.ps_log2, 6), per_chunk = RW_KEYS >> box_log2;
+  const int pack = PACK ? p.pack : 1, heads = p.a.heads / pack;   // an item is one of `heads`
+  const int window = p.a.window, sinks = p.a.sinks, group = heads / pv.H, box_log2 = min(pv.ps_log2, 6), per_chunk = RW_KEYS >> box_log2;
   auto wait_warp = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(b, parity, abort_flag, pv.status)) != 0; };
   // item k of this CTA is in its slot, for the warps that are told: false when the wait gave up
   auto next_item = [&](int k) { return wait_warp(bar(ITEM_FULL + (k & 3)), (uint32_t)((k >> 2) & 1)); };
@@ -200,24 +293,14 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
     if (warp == 0) {
       // ===================== producer: what comes next, and K and V by TMA (lane = (box, half) of the chunk) =====================
       const int n = p.rows.n;
-      // this lane's entry of a group of 32: its first row, rows, pairs of tiles, sequence and length
-      int e_first = 0, e_m = 0, e_pairs = 0, e_seq = -1, e_len = 0, e_group = -1;
-      auto look_up = [&](int i0) {
-        if (i0 == e_group) return;
-        e_group = i0; e_first = e_m = e_pairs = e_len = 0; e_seq = -1;
-        const int i = i0 + lane;
-        if (i >= n) return;
-        e_seq = page_seq_of(pv, p.rows.seqs, i);
-        page_rows_of(p.rows, i, &e_first, &e_m);
-        if (e_seq >= 0) e_len = page_len_of(pv, e_seq);
-        e_pairs = e_m > p.rows.max_rows ? 0 : (e_m + 2 * RW_TILE - 1) / (2 * RW_TILE);
-      };
+      RowsEntries e;
       int total = 0;   // pairs of tiles of all entries
       for (int i0 = 0; i0 < n; i0 += 32) {
-        look_up(i0);
-        total += __reduce_add_sync(0xffffffffu, e_pairs);
-        if (blockIdx.x == 0 && (e_m > p.rows.max_rows || (e_m > 0 && e_seq < 0))) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);   // cannot be answered
+        e.look_up(pv, p.rows, pack, i0);
+        total += __reduce_add_sync(0xffffffffu, e.pairs);
+        if (blockIdx.x == 0 && (e.m > p.rows.max_rows || (e.m > 0 && e.seq < 0))) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);   // cannot be answered
       }
+      const int split = SPLIT ? split_of((long long)total * heads, p.grid) : 1;
       const long long pool_rows = (long long)pv.n_layers * 2 * pv.n_pages * pv.H * pv.ps, plane_rows = (long long)pv.n_pages * pv.H * pv.ps;
       const int box = lane / HALVES, half = lane - box * HALVES;
       const uint32_t place = (uint32_t)(half * RW_BLOCK + ((box << box_log2) * 128));
@@ -225,35 +308,13 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
       uint32_t g = 0;   // chunks of K and V so far
       // works out item k of this CTA and publishes it; the pairs are handed out last first: later rows of a sequence have more keys
       auto publish = [&](int k) {
-        const long long index = blockIdx.x + (long long)k * gridDim.x;
-        const int slot = index < (long long)total * p.a.heads ? total - 1 - (int)(index / p.a.heads) : -1;
+        const long long index = SPLIT && split > 1 ? (k == 0 ? blockIdx.x / split : (long long)total * heads) : blockIdx.x + (long long)k * gridDim.x;
+        const int slot = index < (long long)total * heads ? total - 1 - (int)(index / heads) : -1;
         RowsItem it{};
         it.head = -1;
-        if (slot >= 0) {
-          int before = 0;
-          for (int i0 = 0; i0 < n; i0 += 32) {
-            look_up(i0);
-            int incl = e_pairs;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-              const int v = __shfl_up_sync(0xffffffffu, incl, o);
-              if (lane >= o) incl += v;
-            }
-            const int at = before + incl - e_pairs;
-            const uint32_t here = __ballot_sync(0xffffffffu, slot >= at && slot < at + e_pairs);
-            if (here) {
-              const int src = __ffs(here) - 1;
-              const int skip = (slot - __shfl_sync(0xffffffffu, at, src)) * 2 * RW_TILE, m = __shfl_sync(0xffffffffu, e_m, src);
-              it.head = (int)(index % p.a.heads);
-              it.row0 = __shfl_sync(0xffffffffu, e_first, src) + skip;
-              it.n_rows = min(2 * RW_TILE, m - skip);
-              it.pos0 = __shfl_sync(0xffffffffu, e_len, src) - m + skip;
-              it.seq = __shfl_sync(0xffffffffu, e_seq, src);
-              plan_rows(it, window, sinks, box_log2);
-              break;
-            }
-            before += __shfl_sync(0xffffffffu, incl, 31);
-          }
+        if (slot >= 0 && e.find(pv, p.rows, pack, slot, it)) {
+          plan_rows(it, window, sinks, box_log2, pack);
+          if (!SPLIT || cut_keys(it, split, blockIdx.x)) it.head = (int)(index % heads);
         }
         if (k >= RW_SLOTS && !(ok = wait_warp(bar(ITEM_EMPTY + (k & 3)), (uint32_t)(((k >> 2) & 1) ^ 1)))) return;
         if (lane == 0) {
@@ -290,16 +351,17 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
           if (x >= 2 && !(ok = wait_warp(bar(K_EMPTY + s), ((x >> 1) & 1) ^ 1u))) return;
           load(sK + s * TILE, bar(K_FULL + s), row);
         };
-        if (it.n_chunks > 0) load_k(0, row_of(0, 0));
-        for (int c = 0; c < it.n_chunks && ok; ++c) {   // K a chunk ahead of V: its slot comes free earlier
+        g -= it.template begin<SPLIT>();   // (chunk c of the item is chunk g + c of the CTA)
+        if (it.template end_chunk<SPLIT>() > it.template begin<SPLIT>()) load_k(it.template begin<SPLIT>(), row_of(it.template begin<SPLIT>(), 0));
+        for (int c = it.template begin<SPLIT>(); c < it.template end_chunk<SPLIT>() && ok; ++c) {   // K a chunk ahead of V: its slot comes free earlier
           const uint32_t x = g + c, s = x & 1;
-          const int vrow = row_of(c, 1), krow = c + 1 < it.n_chunks ? row_of(c + 1, 0) : 0;
-          if (c + 1 < it.n_chunks) load_k(c + 1, krow);
+          const int vrow = row_of(c, 1), krow = c + 1 < it.template end_chunk<SPLIT>() ? row_of(c + 1, 0) : 0;
+          if (c + 1 < it.template end_chunk<SPLIT>()) load_k(c + 1, krow);
           if (!ok) break;
           if (x >= 2 && !(ok = wait_warp(bar(V_EMPTY + s), ((x >> 1) & 1) ^ 1u))) break;
           load(sV + s * TILE, bar(V_FULL + s), vrow);
         }
-        g += it.n_chunks;
+        g += it.template end_chunk<SPLIT>();
       }
       if (!ok || *abort_flag) {   // copies already issued land before the CTA's shared memory is given back
         const unsigned long long t0 = now_ns();
@@ -317,7 +379,7 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
         if (!next_item(k) || s_item[k & 3].head < 0) break;
         const RowsItem it = s_item[k & 3];
         auto issue_qk = [&](int tile, int c) {
-          if (c == it.from(tile)) {   // the tile's first of this item
+          if (c == it.template from<SPLIT>(tile)) {   // the tile's first of this item
             if (!wait_warp(bar(Q_FULL + tile), (tile ? ni_b : ni_a) & 1)) return false;
             tc_fence_after();
           }
@@ -333,24 +395,26 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
           __syncwarp();
           return true;
         };
-        if (it.n_chunks > 0) {
-          if (!(ok = wait_warp(bar(K_FULL + (g & 1)), (g >> 1) & 1))) break;
+        g -= it.template begin<SPLIT>();
+        if (it.template end_chunk<SPLIT>() > it.template begin<SPLIT>()) {
+          const uint32_t x = g + it.template begin<SPLIT>();
+          if (!(ok = wait_warp(bar(K_FULL + (x & 1)), (x >> 1) & 1))) break;
           tc_fence_after();
           for (int tile = 0; tile < 2 && ok; ++tile)
-            if (it.active(tile, 0)) ok = issue_qk(tile, 0);
+            if (it.template active<SPLIT>(tile, it.template begin<SPLIT>())) ok = issue_qk(tile, it.template begin<SPLIT>());
           if (!ok) break;
-          if (leader) umma_commit(bar(K_EMPTY + (g & 1)));
+          if (leader) umma_commit(bar(K_EMPTY + (x & 1)));
           __syncwarp();
         }
-        for (int c = 0; c < it.n_chunks && ok; ++c) {
+        for (int c = it.template begin<SPLIT>(); c < it.template end_chunk<SPLIT>() && ok; ++c) {
           const uint32_t x = g + c, s = x & 1;
           if (!(ok = wait_warp(bar(V_OK + s), (x >> 1) & 1))) break;   // V, and the next chunk's K
 #pragma unroll
           for (int tile = 0; tile < 2; ++tile) {
-            if (it.active(tile, c)) {
+            if (it.template active<SPLIT>(tile, c)) {
               const uint64_t vd = desc_mnmajor_v(sV + s * TILE);
               const uint32_t ni = tile ? ni_b : ni_a;
-              if (c == it.from(tile) && ni > 0 && !(ok = wait_warp(bar(O_EMPTY + tile), (ni - 1) & 1))) break;   // the output before has been read
+              if (c == it.template from<SPLIT>(tile) && ni > 0 && !(ok = wait_warp(bar(O_EMPTY + tile), (ni - 1) & 1))) break;   // the output before has been read
               for (int hf = 0; hf < 2; ++hf) {   // the weights come in two halves
                 if (!(ok = wait_warp(bar((hf ? P_FULL : P_HALF) + tile), (tile ? np_b : np_a) & 1))) break;
                 tc_fence_after();
@@ -358,7 +422,7 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
 #pragma unroll
                   for (int kk = 0; kk < RW_KEYS / 32; ++kk)
                     umma_bf16_ts(tmem + 256u + (uint32_t)tile * 128u, tmem + (uint32_t)tile * 128u + (uint32_t)(hf * 4 + kk) * 8u,
-                                 vd + (uint64_t)((hf * 4 + kk) * 128), idesc_pv, (c > it.from(tile) || hf > 0 || kk > 0) ? 1u : 0u);
+                                 vd + (uint64_t)((hf * 4 + kk) * 128), idesc_pv, (c > it.template from<SPLIT>(tile) || hf > 0 || kk > 0) ? 1u : 0u);
                   if (hf && c + 1 == it.to(tile)) umma_commit(bar(O_FULL + tile));
                 }
                 __syncwarp();
@@ -367,16 +431,16 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
               ++(tile ? np_b : np_a);
               if (c + 1 == it.to(tile)) ++(tile ? ni_b : ni_a);
             }
-            if (c + 1 < it.n_chunks && it.active(tile, c + 1) && !(ok = issue_qk(tile, c + 1))) break;
+            if (c + 1 < it.template end_chunk<SPLIT>() && it.template active<SPLIT>(tile, c + 1) && !(ok = issue_qk(tile, c + 1))) break;
           }
           if (!ok) break;
           if (leader) {
             umma_commit(bar(V_EMPTY + s));
-            if (c + 1 < it.n_chunks) umma_commit(bar(K_EMPTY + (s ^ 1)));
+            if (c + 1 < it.template end_chunk<SPLIT>()) umma_commit(bar(K_EMPTY + (s ^ 1)));
           }
           __syncwarp();
         }
-        g += it.n_chunks;
+        g += it.template end_chunk<SPLIT>();
         release_item(k);
       }
     } else {
@@ -387,7 +451,8 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
       for (int k = 0; ok; ++k) {
         if (!next_item(k) || s_item[k & 3].head < 0) break;
         const RowsItem it = s_item[k & 3];
-        for (int c = 0; c < it.n_chunks; ++c) {
+        g -= it.template begin<SPLIT>();
+        for (int c = it.template begin<SPLIT>(); c < it.template end_chunk<SPLIT>(); ++c) {
           const uint32_t x = g + c, s = x & 1;
           const bool all = c >= it.all_from_b && c < it.all_to_a;   // every row of the CTA sees all of the chunk
           if (!(ok = wait_warp(bar(V_FULL + s), (x >> 1) & 1))) break;
@@ -423,11 +488,11 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
           // (the next chunk's K is waited for here: the MMA warp has no time to spare)
-          if (c + 1 < it.n_chunks && !(ok = wait_warp(bar(K_FULL + (s ^ 1)), ((x + 1) >> 1) & 1))) break;
+          if (c + 1 < it.template end_chunk<SPLIT>() && !(ok = wait_warp(bar(K_FULL + (s ^ 1)), ((x + 1) >> 1) & 1))) break;
           __syncwarp();   // (all lanes' zeros and looks before the one arrival)
           if (lane == 0) mbar_arrive(bar(V_OK + s));
         }
-        g += it.n_chunks;
+        g += it.template end_chunk<SPLIT>();
         release_item(k);
       }
     }
@@ -440,17 +505,21 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
     const uint32_t s_addr = tmem + lanes + (uint32_t)tile * 128u, o_addr = s_addr + 256u;
     const float scale2 = p.a.scale * LOG2E;
     const uint64_t scale22 = pair(scale2, scale2);
+    // place x of an item: its row of the call (after row0) and query head (after head * pack)
+    auto row_of = [&](int x) { return PACK ? x / pack : x; };
+    auto sub_of = [&](int x) { return PACK ? x % pack : 0; };
     // the tile's Q, K-major and swizzled: 16-byte piece c of row r lies at piece c ^ (r & 7) of its 128 bytes.  A tile's Q may be
     // overwritten once the scores of its last chunk have been seen.
     auto load_q = [&](const RowsItem& x) {
       constexpr int PIECES = HD / 8, ROWS_PASS = 32 / PIECES;
       const int piece = lane % PIECES, rows = x.n_rows - tile * RW_TILE, r0 = w4 * 32 + lane / PIECES;
-      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.a.q) + (long long)(x.row0 + tile * RW_TILE) * p.a.q_stride + (long long)x.head * HD + piece * 8;
+      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.a.q) + (long long)(x.row0 + (PACK ? 0 : tile * RW_TILE)) * p.a.q_stride + (long long)x.head * pack * HD + piece * 8;
       const uint32_t dst = sQ + tile * TILE + (piece >> 3) * RW_BLOCK;
 #pragma unroll 4
       for (int i = 0; i < 32 / ROWS_PASS; ++i) {
         const int r = r0 + i * ROWS_PASS;
-        cp_async16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), q + (long long)(r < rows ? r : 0) * p.a.q_stride, r < rows);
+        const int at = PACK ? tile * RW_TILE + (r < rows ? r : 0) : r < rows ? r : 0;
+        cp_async16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), q + (long long)row_of(at) * p.a.q_stride + sub_of(at) * HD, r < rows);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -462,22 +531,22 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
     };
     uint32_t n_s = 0, n_item = 0;   // chunks and items that the tile has worked on
     bool ok = next_item(0), more = ok && s_item[0].head >= 0;
-    if (more && s_item[0].has(tile)) { load_q(s_item[0]); q_loaded(); }
+    if (more && s_item[0].template has<SPLIT>(tile)) { load_q(s_item[0]); q_loaded(); }
     for (int k = 0; ok && more; ++k) {
       const RowsItem& it = s_item[k & 3];
-      const int head = it.head, from = it.from(tile), to = it.to(tile), first = it.first, skew = it.skew;
+      const int head = it.head, from = it.template from<SPLIT>(tile), to = it.to(tile), first = it.first, skew = it.skew;
       const int t_rows = min(RW_TILE, it.n_rows - tile * RW_TILE);   // rows of the tile, <= 0: none
       const bool valid = t < t_rows, has = to > from;
-      const int row0 = it.row0 + tile * RW_TILE, pos0 = it.pos0 + tile * RW_TILE;
+      const int place0 = PACK ? tile * RW_TILE : 0, row0 = it.row0 + (PACK ? 0 : tile * RW_TILE), pos0 = it.pos0 + (PACK ? 0 : tile * RW_TILE);
       const int all_from = tile ? it.all_from_b : it.all_from, all_to = tile ? it.all_to_b : it.all_to_a;
-      const int pos = valid ? pos0 + t : -1, lo = window > 0 ? pos - window + 1 : 0;   // sees [lo, pos] and the sinks
+      const int pos = valid ? pos0 + row_of(place0 + t) : -1, lo = window > 0 ? pos - window + 1 : 0;   // sees [lo, pos] and the sinks
       float m = -INFINITY, l = 0.f;
       bool next_q = false;
       auto look_ahead = [&]() {   // what comes next, and its Q on the way
         if (!next_item(k + 1)) return false;
         const RowsItem& next = s_item[(k + 1) & 3];
         more = next.head >= 0;
-        next_q = more && next.has(tile);
+        next_q = more && next.template has<SPLIT>(tile);
         if (next_q) load_q(next);
         return true;
       };
@@ -570,12 +639,29 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
       if (next_q) q_loaded();   // the next scores are worked on while this output is finished
       if (has && !(ok = wait_warp(bar(O_FULL + tile), n_item & 1))) break;
       const bool unclean = *reinterpret_cast<volatile int*>(&s_item[k & 3].unclean) != 0;
-      if (t_rows > 0 && !unclean) {
+      const int part = SPLIT ? it.part : -1;
+      if (t_rows > 0 && part >= 0) {   // for rows_join_kernel
+        float* mine = p.parts + (size_t)part * rows_part_floats<HD>();
+        if (has && !unclean) {
+          tc_fence_after();
+#pragma unroll 1
+          for (int g = 0; g < HD / 16; ++g) {
+            uint32_t ov[16];
+            tmem_ld16(o_addr + g * 16, ov);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              reinterpret_cast<uint4*>(mine)[(g * 4 + j) * RW_ROWS + tile * RW_TILE + t] = make_uint4(ov[4 * j], ov[4 * j + 1], ov[4 * j + 2], ov[4 * j + 3]);
+          }
+        }
+        reinterpret_cast<float2*>(mine + RW_ROWS * HD)[tile * RW_TILE + t] = make_float2(m, unclean ? __uint_as_float(0x7fffffffu) : l);
+      }
+      if (t_rows > 0 && part < 0 && !unclean) {
         tc_fence_after();
         const float inv = l == 0.f ? 0.f : 1.f / l;
         // through shared memory, so that a store covers 128 bytes of each of four rows (16 bytes of 32 rows cost 9000 cycles a tile)
         uint8_t* mine = gen + (sO - base) + (warp - 4) * RW_STAGE_OUT;
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + (long long)(row0 + w4 * 32) * p.a.out_stride + (long long)head * HD + (lane & 7) * 8;
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.a.out) + (long long)(row0 + (PACK ? 0 : w4 * 32)) * p.a.out_stride + (long long)head * pack * HD + (lane & 7) * 8;
 #pragma unroll 1
         for (int g = 0; g < HD / 64; ++g) {   // (short loops: this code runs once an item, and what it costs is its fetch)
 #pragma unroll 1
@@ -599,12 +685,13 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
 #pragma unroll 4
           for (int i = 0; i < 8; ++i) {
             const int r = i * 4 + (lane >> 3);
+            const int at = PACK ? place0 + w4 * 32 + r : r;
             if (w4 * 32 + r < t_rows)
-              *reinterpret_cast<uint4*>(out + (long long)r * p.a.out_stride + g * 64) = *reinterpret_cast<const uint4*>(mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+              *reinterpret_cast<uint4*>(out + (long long)row_of(at) * p.a.out_stride + sub_of(at) * HD + g * 64) = *reinterpret_cast<const uint4*>(mine + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
           }
           __syncwarp();
         }
-        if (valid && p.a.lse) p.a.lse[(long long)(row0 + t) * p.a.heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+        if (valid && p.a.lse) p.a.lse[(long long)(row0 + row_of(place0 + t)) * p.a.heads + head * pack + sub_of(place0 + t)] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
       }
       if (has) {
         tc_fence_before();
@@ -612,17 +699,18 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
         if (lane == 0) mbar_arrive(bar(O_EMPTY + tile));
         ++n_item;
       }
-      if (t_rows > 0 && unclean) {
+      if (t_rows > 0 && part < 0 && unclean) {
         for (int x = w4 * 32; x < min(t_rows, w4 * 32 + 32); ++x) {   // (rare) the warp's rows, one after another
-          const long long row = row0 + x;
+          const long long row = row0 + row_of(place0 + x);
+          const int mine = head * pack + sub_of(place0 + x);
           float q[HD / 32], o[HD / 32], rm = -INFINITY, rl = 0.f;
 #pragma unroll
           for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
-          load_dims(reinterpret_cast<const __nv_bfloat16*>(p.a.q) + row * p.a.q_stride + (long long)head * HD + lane * (HD / 32), q);
-          if (pos0 + x >= 0)
-            attend_row_warp<__nv_bfloat16, HD>(pv, p.a.layer, pv.table + (size_t)it.seq * pv.max_pages, head / group, pos0 + x, window, sinks, scale2, q,
+          load_dims(reinterpret_cast<const __nv_bfloat16*>(p.a.q) + row * p.a.q_stride + (long long)mine * HD + lane * (HD / 32), q);
+          if (pos0 + row_of(place0 + x) >= 0)
+            attend_row_warp<__nv_bfloat16, HD>(pv, p.a.layer, pv.table + (size_t)it.seq * pv.max_pages, head / group, pos0 + row_of(place0 + x), window, sinks, scale2, q,
                                                o, &rm, &rl);
-          store_row_warp<__nv_bfloat16, HD>(p.a, row, head, o, rm, rl);
+          store_row_warp<__nv_bfloat16, HD>(p.a, row, mine, o, rm, rl);
         }
       }
       release_item(k);
@@ -637,21 +725,140 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
   }
 }
 
-}  // namespace
+// The parts of items whose keys several CTAs shared: grid (item, 32 of its rows), a thread a row and four of its dimensions at a time.
+constexpr int JOIN_THREADS = 256;
 
-cudaError_t pages_rows_prepare(int hd) {
-  return hd == 64 ? cudaFuncSetAttribute(pages_rows_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem<64>())
-                  : cudaFuncSetAttribute(pages_rows_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem<128>());
+template <int HD>
+__global__ void __launch_bounds__(JOIN_THREADS) rows_join_kernel(const RowsParams p) {
+  constexpr int WARPS = JOIN_THREADS / 32, PER = HD / 4 / WARPS, PITCH = HD + 8;
+  __shared__ __align__(16) __nv_bfloat16 s_out[32 * PITCH];
+  __shared__ uint32_t s_alone;
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const PageView& pv = p.pv;
+  const int window = p.a.window, sinks = p.a.sinks, pack = p.pack, heads = p.a.heads / pack;
+  RowsEntries e;
+  int total = 0;
+  for (int i0 = 0; i0 < p.rows.n; i0 += 32) {
+    e.look_up(pv, p.rows, pack, i0);
+    total += __reduce_add_sync(0xffffffffu, e.pairs);
+  }
+  RowsItem it{};
+  if ((long long)blockIdx.x < (long long)total * heads && e.find(pv, p.rows, pack, total - 1 - (int)(blockIdx.x / heads), it))
+    plan_rows(it, window, sinks, min(pv.ps_log2, 6), pack);   // (else no rows)
+  pdl_wait();
+  const int split = split_of((long long)total * heads, p.grid), n = parts_of(it, split), head0 = (int)(blockIdx.x % heads) * pack, x0 = blockIdx.y * 32, here = min(32, it.n_rows - x0);
+  if (n == 1 || here <= 0) return;   // (written by the one CTA that worked on it)
+  const int x = x0 + lane;
+  const float* part0 = p.parts + (size_t)blockIdx.x * split * rows_part_floats<HD>();
+  float m[RW_MAX_SPLIT], M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int s = 0; s < RW_MAX_SPLIT; ++s) {
+    const float2 st = s < n && lane < here ? reinterpret_cast<const float2*>(part0 + (size_t)s * rows_part_floats<HD>() + RW_ROWS * HD)[x] : make_float2(-INFINITY, 0.f);
+    m[s] = st.y == 0.f ? -INFINITY : st.x;   // (no key of the part: nothing has been left)
+    M = fmaxf(M, m[s]);
+  }
+  const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+  for (int s = 0; s < RW_MAX_SPLIT; ++s) {
+    const float l = s < n && lane < here ? reinterpret_cast<const float2*>(part0 + (size_t)s * rows_part_floats<HD>() + RW_ROWS * HD)[x].y : 0.f;
+    const float f = l == 0.f ? 0.f : fast_exp2(m[s] - ref);
+    L = fmaf(f, l, L);
+    m[s] = f;
+  }
+  const uint32_t alone = __ballot_sync(0xffffffffu, L != L);   // rows that see NaN or infinities, or whose part met some
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int g = warp * PER + k;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int s = 0; s < RW_MAX_SPLIT; ++s) {
+      if (s < n && m[s] != 0.f && lane < here) {
+        const float4 o = reinterpret_cast<const float4*>(part0 + (size_t)s * rows_part_floats<HD>())[g * RW_ROWS + x];
+        v.x = fmaf(m[s], o.x, v.x); v.y = fmaf(m[s], o.y, v.y); v.z = fmaf(m[s], o.z, v.z); v.w = fmaf(m[s], o.w, v.w);
+      }
+    }
+    *reinterpret_cast<uint2*>(&s_out[lane * PITCH + g * 4]) = make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
+  }
+  if (threadIdx.x == 0) s_alone = alone;
+  __syncthreads();
+  constexpr int PIECES = HD / 8;
+  for (int i = threadIdx.x; i < here * PIECES; i += JOIN_THREADS) {
+    const int r = i / PIECES, c = i - r * PIECES;
+    if ((s_alone >> r) & 1u) continue;
+    *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.a.out) + (long long)(it.row0 + (x0 + r) / pack) * p.a.out_stride + (long long)(head0 + (x0 + r) % pack) * HD + c * 8) =
+        *reinterpret_cast<const uint4*>(&s_out[r * PITCH + c * 8]);
+  }
+  if (warp == 0 && lane < here && p.a.lse && !((alone >> lane) & 1u))
+    p.a.lse[(long long)(it.row0 + x / pack) * p.a.heads + head0 + x % pack] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+  for (int r = warp; r < here; r += WARPS) {
+    if (!((alone >> r) & 1u)) continue;
+    const int token = (x0 + r) / pack, head = head0 + (x0 + r) % pack;
+    const long long row = it.row0 + token;
+    float q[HD / 32], o[HD / 32], rm = -INFINITY, rl = 0.f;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
+    load_dims(reinterpret_cast<const __nv_bfloat16*>(p.a.q) + row * p.a.q_stride + (long long)head * HD + lane * (HD / 32), q);
+    if (it.pos0 + token >= 0)
+      attend_row_warp<__nv_bfloat16, HD>(pv, p.a.layer, pv.table + (size_t)it.seq * pv.max_pages, head / (p.a.heads / pv.H), it.pos0 + token, window, sinks,
+                                         p.a.scale * LOG2E, q, o, &rm, &rl);
+    store_row_warp<__nv_bfloat16, HD>(p.a, row, head, o, rm, rl);
+  }
 }
 
-// map: the pool as [rows][head_dim], boxes of min(page_size, 64) rows and 64 columns.  sms: CTAs at most.
-cudaError_t launch_pages_rows(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, int sms, cudaStream_t st) {
+}  // namespace
+
+size_t pages_rows_part_bytes(const PageView& pv, int grid) {
+  return pv.es == 2 ? (size_t)grid * (pv.hd == 64 ? rows_part_floats<64>() : rows_part_floats<128>()) * 4 : 0;
+}
+
+// Calls f(kernel, shared memory) for each form of the kernel.
+template <typename F> static cudaError_t for_rows_kernels(int hd, F f) {
+  cudaError_t e = cudaSuccess;
+  auto forms = [&](auto hd_c) {
+    constexpr int HD = decltype(hd_c)::value;
+    e = f(false, false, pages_rows_kernel<HD, false, false>, rows_smem<HD>());
+    if (e == cudaSuccess) e = f(true, false, pages_rows_kernel<HD, true, false>, rows_smem<HD>());
+    if (e == cudaSuccess) e = f(false, true, pages_rows_kernel<HD, false, true>, rows_smem<HD>());
+    if (e == cudaSuccess) e = f(true, true, pages_rows_kernel<HD, true, true>, rows_smem<HD>());
+  };
+  hd == 64 ? forms(std::integral_constant<int, 64>{}) : forms(std::integral_constant<int, 128>{});
+  return e;
+}
+
+cudaError_t pages_rows_prepare(int hd) {
+  return for_rows_kernels(hd, [](bool, bool, auto kernel, size_t smem) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+}
+
+// map: the pool as [rows][head_dim], boxes of min(page_size, 64) rows and 64 columns.  parts: pages_rows_part_bytes.  sms: CTAs at most.
+cudaError_t launch_pages_rows(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int sms, int* launches,
+                              cudaStream_t st) {
   RowsParams p;
-  p.pv = pv; p.rows = rows; p.a = a;
-  const long long items = (rows.n_rows / (2 * RW_TILE) + (long long)rows.n) * a.heads;   // at most
-  const unsigned grid = (unsigned)(items < sms ? items : sms);
-  if (pv.hd == 64) launch_pdl(pages_rows_kernel<64>, grid, RW_THREADS, rows_smem<64>(), st, *(const CUtensorMap*)map, p);
-  else launch_pdl(pages_rows_kernel<128>, grid, RW_THREADS, rows_smem<128>(), st, *(const CUtensorMap*)map, p);
+  p.pv = pv; p.rows = rows; p.a = a; p.parts = (float*)parts;
+  const long long rows_most = rows.max_rows < rows.n_rows ? rows.max_rows : rows.n_rows;   // rows of an entry that is answered
+  const int group = a.heads / pv.H;
+  p.pack = group > 1 && rows_most * group <= RW_ROWS ? group : 1;
+  const int heads = a.heads / p.pack;
+  // items at most, and about (their number stands on the device; with fewer, the form that does not share answers as well)
+  const long long most = p.pack > 1 ? (long long)rows.n * heads : (rows.n_rows + (long long)(RW_ROWS - 1) * rows.n) / RW_ROWS * heads;
+  const long long filled = ((long long)rows.n_rows * p.pack + RW_ROWS - 1) / RW_ROWS, about = (filled > rows.n ? filled : rows.n) * heads;
+  const bool split = about * 2 <= sms, pack = p.pack > 1;
+  // (no more CTAs than can share: rows_join_kernel's begin beside them on SMs that are left, 1.5 us)
+  const long long ctas = split && most * 2 <= sms ? most * (sms / most < RW_MAX_SPLIT ? sms / most : RW_MAX_SPLIT) : split ? sms : most;
+  p.grid = (int)(ctas < sms ? ctas : sms);
+  const cudaError_t e = for_rows_kernels(pv.hd, [&](bool split_form, bool pack_form, auto kernel, size_t smem) {
+    if (pack_form != pack || split_form != split) return cudaSuccess;
+    launch_pdl(kernel, p.grid, RW_THREADS, smem, st, *(const CUtensorMap*)map, p);
+    ++*launches;
+    return cudaGetLastError();
+  });
+  if (e || !split) return e;
+  const dim3 join((unsigned)(most < p.grid / 2 ? most : p.grid / 2), (unsigned)(rows_most * p.pack < RW_ROWS ? (rows_most * p.pack + 31) / 32 : RW_ROWS / 32));
+  if (join.x == 0) return e;
+  if (pv.hd == 64) launch_pdl(rows_join_kernel<64>, join, JOIN_THREADS, 0, st, p);
+  else launch_pdl(rows_join_kernel<128>, join, JOIN_THREADS, 0, st, p);
+  ++*launches;
   return cudaGetLastError();
 }
 

@@ -339,3 +339,95 @@ def test_refused_heads():
         assert e.value.code == 2
     wide = torch.randn(1, 1024, 64, device="cuda:0").bfloat16()
     compare(cache.attention(0, wide), None, wide, keys, values, [20], [1], 0, 0)
+
+
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(4, 2, 128), (16, 1, 128), (3, 3, 64), (40, 8, 128)])
+@pytest.mark.parametrize("lens,rows", [([9000], [17]), ([5000], [256]), ([4099], [130]), ([3000, 40, 6001, 1, 0], [33, 40, 256, 1, 0])])
+def test_few_rows_over_long_contexts(heads, kv_heads, head_dim, lens, rows):
+    """Several CTAs share the keys of a query head's rows; some of the sequences are too short for that."""
+    run(lens, rows, heads, kv_heads, head_dim, 64, "bf16", seed=heads + len(lens))
+
+
+@pytest.mark.parametrize("window,sinks,page", [(2000, 0, 16), (2000, 70, 64), (1100, 5, 128), (4999, 300, 32)])
+def test_few_rows_of_long_windows(window, sinks, page):
+    run([7000, 2500], [200, 90], 6, 2, 128, page, "bf16", window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, 3.3e38])
+def test_few_rows_over_long_contexts_with_anything_in_hidden_places(bad):
+    """Keys and values behind a row's place and before its window hold anything; a value that some rows see reaches them alone."""
+    lens, rows, window = [5000], [150], 3000
+    cache, table, q, keys, values = build(lens, rows, 4, 2, 128, 64, "bf16")
+    kw = dict(row_off=dev(np.array([0, 150])), max_rows=150, window=window)
+    want = cache.attention(0, q, **kw)
+    compare(want, None, q, keys, values, lens, rows, window, 0)
+    for x in (keys[0], values[0]):
+        x[:5000 - 150 - window] = bad           # before every row's window
+    put(cache, table, 0, 0, keys[0], values[0], 0)
+    assert torch.equal(cache.attention(0, q, **kw), want)
+    values[0][4900] = bad                       # position 4900: rows 50 .. 149 see it, 0 .. 49 do not
+    put(cache, table, 0, 4900, keys[0][4900:4901], values[0][4900:4901], 0)
+    lse = torch.zeros(150, 4, device="cuda:0")
+    got = cache.attention(0, q, lse=lse, **kw)
+    cache.poll()
+    if not math.isfinite(bad):
+        assert not torch.isfinite(got[50:]).any() and torch.isfinite(lse).all()
+    v = torch.where(torch.isfinite(values[0].float()), values[0].float(), 0.0)
+    v[:5000 - 150 - window] = 0
+    k = keys[0].clone()
+    k[:5000 - 150 - window] = 0
+    ref, _, absv, absqk = attend(q[:50], k, v.to(torch.bfloat16), np.arange(4850, 4900), window, 0, None)
+    tol = tolerance(q.dtype, ref, absv, absqk, 5000, 1 / math.sqrt(128))
+    assert ((got[:50].double() - ref).abs() <= tol).all()
+
+
+def test_few_rows_of_many_sequences_in_a_graph():
+    """The parts of one call are joined before the next one's are left; the same again in a replay."""
+    lens, rows = [2600, 1800, 3000], [20, 33, 7]
+    cache, table, q, keys, values = build(lens, rows, 8, 2, 128, 32, "bf16")
+    kw = dict(row_off=dev(np.array([0, 20, 53, 60])), max_rows=33)
+    outs = [torch.empty_like(q) for _ in range(3)]
+    want = cache.attention(0, q, **kw).clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for i, o in enumerate(outs):
+            cache.attention(0, q if i != 1 else -q, out=o, **kw)
+    for _ in range(3):
+        for o in outs:
+            o.fill_(7)
+        g.replay()
+        assert torch.equal(outs[0], want) and torch.equal(outs[2], want)
+        compare(outs[1], None, -q, keys, values, lens, rows, 0, 0)
+    cache.poll()
+
+
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(8, 2, 128), (32, 1, 128), (6, 2, 64), (28, 4, 128)])
+@pytest.mark.parametrize("rows,window,sinks", [([6, 1, 8, 0, 3], 0, 0), ([8, 8, 8, 8, 8], 500, 5), ([7, 2, 5, 1, 1], 130, 0)])
+@pytest.mark.parametrize("page", [16, 128])
+def test_few_rows_of_grouped_heads(heads, kv_heads, head_dim, rows, window, sinks, page):
+    """The query heads of a key and value head share a tile; contexts that are shared out and such that are not."""
+    run([3000, 1, 1400, 0, 257] if rows[0] != 8 else [3000, 8, 1400, 9, 257], rows, heads, kv_heads, head_dim, page, "bf16", window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("rows", [33, 64, 65])
+def test_rows_of_grouped_heads_in_one_tile_and_two(rows):
+    """Four heads of 33 to 64 rows fill both tiles of an item; those of 65 rows do not fit one."""
+    run([700, 1500], [rows, rows - 1], 8, 2, 128, 64, "bf16")
+    run([700, 1500], [rows, rows - 1], 8, 2, 128, 64, "bf16", window=90, sinks=2)
+
+
+def test_few_rows_of_grouped_heads_beside_what_they_must_not_touch():
+    """Strided rows, rows behind the last sequence, NaN in values that some rows do not see."""
+    lens, rows = [2000, 300], [5, 4]
+    cache, table, q, keys, values = build(lens, rows, 8, 2, 128, 32, "bf16")
+    values[1][298] = math.nan            # position 298: the last two rows of sequence 1
+    put(cache, table, 1, 0, keys[1], values[1], 0)
+    wide = torch.full((12, 24, 128), 5.0, device="cuda:0", dtype=torch.bfloat16)
+    wide[:9, :8] = q
+    out = torch.full((12, 24, 128), 3.0, device="cuda:0", dtype=torch.bfloat16)
+    cache.attention(0, wide[:, :8], out=out[:, 8:16], row_off=dev(np.array([0, 5, 9])), max_rows=5)
+    cache.poll()
+    assert (out[9:] == 3).all() and (out[:, :8] == 3).all() and (out[:, 16:] == 3).all()
+    assert torch.isnan(out[7:9, 8:16]).all()
+    compare(out[:5, 8:16], None, q[:5], keys[:1], values[:1], lens[:1], [5], 0, 0)
+    compare(out[5:7, 8:16], None, q[5:7], [keys[1][:298]], [values[1][:298]], [298], [2], 0, 0)
