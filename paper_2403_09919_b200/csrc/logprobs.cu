@@ -366,9 +366,10 @@ __global__ void __launch_bounds__(LP_THREADS, sizeof(T) == 2 ? 3 : 0) logprob_ke
 }  // namespace
 
 cudaError_t launch_logprobs(int dtype, const LogprobArgs& a, cudaStream_t st) {
-  // CTAs per row: enough to fill the SMs when there are few rows
+  // CTAs per row: more than one where rows are long and few.  Fp32, us with 1, 2, 4, 8: 6 x 32000 6.0, 6.4, 6.2, 7.4; 6 x 64000 8.3,
+  // 7.6, 6.9, 7.4; 6 x 128000 12.9, 10.0, 8.2, 8.1; 74 x 64000 8.6, 8.0, 9.9, 16.8; 148 x 32000 6.4, 9.3, 14.4, 29.7.
   int S = 1;
-  while (S < 8 && (long long)a.rows * S < 2 * 148 && a.vocab / (2 * S) >= LP_THREADS * 4) S *= 2;
+  while (S < 8 && (long long)a.rows * S * 2 <= 148 && a.vocab / (2 * S) >= 16384) S *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)a.rows * S);
   cfg.blockDim = LP_THREADS;
