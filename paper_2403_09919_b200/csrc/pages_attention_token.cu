@@ -15,6 +15,9 @@
 //     What they hold is joined in shared memory at the end of an item.
 //   - An item that crosses CTAs leaves its parts (unscaled output, maximum, sum, fp32) in the workspace; the last CTA to
 //     arrive joins them in the order of the CTAs, so that the result does not depend on who is last.
+// Measured with the write of the tokens' K and V before it (a launch of its own, 4 us of these): 16 sequences, 296 MB of K and V,
+// 61.6 us (4.8 TB/s); 1.29 GB 206 us (6.3 TB/s, 0.96 of a copy); a window of 254 MB 53 us; one sequence of 900 tokens (14.8 MB)
+// 10.2 us, a chain of latencies: the write's, three looks into the tables, a page's copy, the products, the join.
 // Keys outside the row's sight are masked by selection and their V is replaced by zeros bit by bit: they may hold anything.
 #include <cuda.h>
 
@@ -32,7 +35,11 @@ constexpr int TK_KEYS = 64;          // keys of a chunk
 constexpr int TK_WARPS = 4;          // consumer warps, 16 keys each
 constexpr int TK_THREADS = TK_WARPS * 32 + 32;
 constexpr int TK_STAGES = 6;
-constexpr int TK_MIN_UNITS = 3;      // units a CTA takes at least
+// Units that a CTA takes at least where an item is cut, and chunks of an item that is not: the more rows a part has, the longer the
+// join of many (900 tokens of 32 heads: 8.3 us with 3, 8.7 with 4, 10.0 with 6; 16384 tokens of 16 query heads on one: 27.1 with 6,
+// 20.7 with 10; fp32, whose chunks take longer, 1000 tokens of 4 heads: 9.7 with 1, 12.5 with 3).
+constexpr int TK_MIN_UNITS = 3, TK_MIN_UNITS_WIDE = 10, TK_WHOLE = 10;
+constexpr int TK_JOIN = 16;          // parts that a thread of the join has under way
 
 struct TokenParams {
   PageView pv;
@@ -96,6 +103,7 @@ struct Share {
 struct ShareScratch {
   long long before;            // chunks before the CTA's first entry
   long long scan[TK_WARPS + 1];
+  int filled[TK_WARPS + 1];
   int entry, last;             // that entry; whether this CTA joins an item's parts
 };
 
@@ -112,7 +120,21 @@ __device__ __forceinline__ long long mul_div(long long a, int b, long long c) {
   return a * b / c;
 }
 
-__device__ __forceinline__ Share share_of(const TokenParams& p, int items, ShareScratch& sc) {
+// CTAs that take part: T units in `all` items of C = T / all chunks on average.  Where items are as long as each other the cuts then
+// fall on their ends, so that a CTA leaves one part and joins once (one sequence of 900 tokens, 32 heads: 9.3 us in 3 CTAs an item,
+// 13.5 over all 148; 300 tokens: 6.1 an item a CTA, 7.8 over all).
+__device__ __forceinline__ int ctas_for(long long T, long long all, int grid, int min_units, int whole) {
+  if (T <= 0) return 0;
+  if (all <= grid) {
+    const int items = (int)all, C = (int)min(T / items, 1ll << 20);
+    return items * (C <= whole ? 1 : max(1, min(grid / items, C / min_units)));
+  }
+  // whole items where that costs the longest CTA four units at most (16 sequences of 200 tokens, 32 heads: 15.2 us, cut 17.8)
+  const long long per = (all + grid - 1) / grid;
+  return all % per == 0 && per * T <= (T / grid + 4) * all ? (int)(all / per) : grid;
+}
+
+__device__ __forceinline__ Share share_of(const TokenParams& p, int items, int min_units, int whole, ShareScratch& sc) {
   Share sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (p.rows.n <= 32) {   // a lane per entry, every warp for itself (one user's 900 tokens: 0.8 us less than over the CTA's memory)
@@ -126,7 +148,7 @@ __device__ __forceinline__ Share share_of(const TokenParams& p, int items, Share
       if (lane >= o) incl += v;
     }
     sh.T = (long long)__shfl_sync(0xffffffffu, incl, 31) * items;
-    sh.G = (int)min((long long)gridDim.x, (sh.T + TK_MIN_UNITS - 1) / TK_MIN_UNITS);
+    sh.G = ctas_for(sh.T, (long long)__popc(__ballot_sync(0xffffffffu, s.chunks > 0)) * items, gridDim.x, min_units, whole);
     sh.n_units = 0;
     const int c = blockIdx.x;
     if (c == 0 && warp == 0 && lane < p.rows.n) report_entry(p, lane);
@@ -149,26 +171,32 @@ __device__ __forceinline__ Share share_of(const TokenParams& p, int items, Share
   }
   const int per = (p.rows.n + TK_THREADS - 1) / TK_THREADS, e0 = min((int)threadIdx.x * per, p.rows.n), e1 = min(e0 + per, p.rows.n);
   long long mine = 0;
+  int filled = 0;
   for (int i = e0; i < e1; ++i) {
     int seq, row;
-    mine += span_of(p, i, &seq, &row).chunks;
+    const int n = span_of(p, i, &seq, &row).chunks;
+    mine += n;
+    filled += n > 0;
   }
+  filled = __reduce_add_sync(0xffffffffu, filled);
   long long before = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const long long v = __shfl_up_sync(0xffffffffu, before, o);
     if (lane >= o) before += v;
   }
-  if (lane == 31) sc.scan[warp] = before;
+  if (lane == 31) { sc.scan[warp] = before; sc.filled[warp] = filled; }
   __syncthreads();
   long long chunks = 0;
   before -= mine;
+  filled = 0;
   for (int w = 0; w <= TK_WARPS; ++w) {
     if (w < warp) before += sc.scan[w];
     chunks += sc.scan[w];
+    filled += sc.filled[w];
   }
   sh.T = chunks * items;
-  sh.G = (int)min((long long)gridDim.x, (sh.T + TK_MIN_UNITS - 1) / TK_MIN_UNITS);
+  sh.G = ctas_for(sh.T, (long long)filled * items, gridDim.x, min_units, whole);
   sh.n_units = 0;
   const int c = blockIdx.x;
   if (c == 0)
@@ -204,6 +232,8 @@ __device__ __forceinline__ int cta_of_unit(long long unit, long long T, int G) {
   return (int)(((unit + 1) * G - 1) / T);
 }
 
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TK_WARPS * 32) : "memory"); }
+
 // The warps' outputs (s_out [TK_WARPS][R][HD + 4]), maxima and sums (s_stat) joined into the output, or into this CTA's part of an
 // item that it shares: by all consumers, 4 dimensions a thread.
 template <typename T, int HD, int R>
@@ -238,7 +268,8 @@ __device__ __forceinline__ void join_warps(const TokenParams& p, const float* s_
   }
 }
 
-// The parts of an item joined in the order of its CTAs, by the consumers of the last one to arrive.
+// The parts of an item joined in the order of its CTAs, by the consumers of the last one to arrive: TK_JOIN parts' loads under way at
+// a time, the last batch filled up with its last part (a rest one by one took 0.4 us for each; 18 parts: 11.5 us, with it 13.2).
 template <typename T, int HD>
 __device__ __forceinline__ void join_parts(const TokenParams& p, int first_cta, int last_cta, int row_out, long long head0, int q_rows) {
   constexpr int PITCH = HD + 4;
@@ -249,20 +280,34 @@ __device__ __forceinline__ void join_parts(const TokenParams& p, int first_cta, 
     const float* at = p.parts + (size_t)(first_cta + 1) * step + row * PITCH;
     const int others = last_cta - first_cta;
     float M = __ldcg(at0 + HD);
-#pragma unroll 8
-    for (int k = 0; k < others; ++k) M = fmaxf(M, __ldcg(at + k * step + HD));
+    for (int k0 = 0; k0 < others; k0 += TK_JOIN) {
+      float x[TK_JOIN];
+#pragma unroll
+      for (int k = 0; k < TK_JOIN; ++k) x[k] = __ldcg(at + min(k0 + k, others - 1) * step + HD);
+#pragma unroll
+      for (int k = 0; k < TK_JOIN; ++k) M = fmaxf(M, x[k]);
+    }
     const float ref = M == -INFINITY ? 0.f : M;
     float f = fast_exp2(__ldcg(at0 + HD) - ref);
     float L = f * __ldcg(at0 + HD + 1);
     float4 v = __ldcg(reinterpret_cast<const float4*>(at0 + d));
     v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-#pragma unroll 8
-    for (int k = 0; k < others; ++k) {
-      const float2 st = __ldcg(reinterpret_cast<const float2*>(at + k * step + HD));
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(at + k * step + d));
-      f = fast_exp2(st.x - ref);
-      L = fmaf(f, st.y, L);
-      v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+    for (int k0 = 0; k0 < others; k0 += TK_JOIN) {
+      float2 st[TK_JOIN];
+      float4 x[TK_JOIN];
+#pragma unroll
+      for (int k = 0; k < TK_JOIN; ++k) {
+        const float* part = at + min(k0 + k, others - 1) * step;
+        st[k] = __ldcg(reinterpret_cast<const float2*>(part + HD));
+        x[k] = __ldcg(reinterpret_cast<const float4*>(part + d));
+      }
+#pragma unroll
+      for (int k = 0; k < TK_JOIN; ++k) {
+        if (k0 + k >= others) break;
+        f = fast_exp2(st[k].x - ref);
+        L = fmaf(f, st[k].y, L);
+        v.x = fmaf(f, x[k].x, v.x); v.y = fmaf(f, x[k].y, v.y); v.z = fmaf(f, x[k].z, v.z); v.w = fmaf(f, x[k].w, v.w);
+      }
     }
     const float inv = L == 0.f ? 0.f : 1.f / L;
     T* out = reinterpret_cast<T*>(p.a.out) + (long long)row_out * p.a.out_stride + (head0 + row) * HD + d;
@@ -299,7 +344,6 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(TK_WARPS * 32) : "memory"); }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
@@ -340,7 +384,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
   pdl_enter();
 
   const int items = pv.H * p.tiles, c = blockIdx.x;
-  const Share sh = share_of(p, items, share);
+  const Share sh = share_of(p, items, WIDE ? TK_MIN_UNITS_WIDE : TK_MIN_UNITS, TK_WHOLE, share);
   if (sh.n_units == 0) return;
   Cursor cur = sh.first;
   const int n_units = sh.n_units, G = sh.G;
@@ -549,7 +593,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_f32_kernel(const To
   __syncthreads();
   pdl_enter();
   const int items = pv.H * p.tiles, c = blockIdx.x;
-  const Share sh = share_of(p, items, share);
+  const Share sh = share_of(p, items, 1, 1, share);
   if (sh.n_units == 0) return;
   Cursor cur = sh.first;
   const int n_units = sh.n_units, G = sh.G;
