@@ -79,6 +79,7 @@ size_t pages_rows_part_bytes(const PageView& pv, int grid);
 cudaError_t launch_pages_rows(const void* map, const PageView& pv, const PageRows& rows, const PageAttention& a, void* parts, int sms, int* launches,
                               cudaStream_t st);
 // many rows per sequence, fp32
+cudaError_t pages_attention_fp32_prepare(int hd);
 cudaError_t launch_pages_attention_fp32(const PageView& pv, const PageRows& rows, const PageAttention& a, cudaStream_t st);
 
 // ---- pages_api.cu: a handle for the engine's own passes (rd_handle), which prompts and autoregressive steps may run on

@@ -201,6 +201,7 @@ int redrafter_pages_init(const rd_page_cache* cache, void* workspace, size_t ws_
     }
     e = pages_rows_prepare(pv.hd);
   }
+  if (e == cudaSuccess && pv.es == 4) e = pages_attention_fp32_prepare(pv.hd);
   if (e == cudaSuccess) e = pages_token_prepare(pv);
   if (e == cudaSuccess) e = cudaMemsetAsync(h->parts, 0, pages_token_part_bytes(pv, TOKEN_MAX_GRID), 0);
   if (e == cudaSuccess) e = cudaMemsetAsync(workspace, 0, 256, 0);

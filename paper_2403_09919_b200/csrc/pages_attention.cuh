@@ -14,20 +14,53 @@ __device__ __forceinline__ void visible_keys(int pos, int window, int sinks, int
   *sink_end = min(sinks, *start);
 }
 
-// Entry of the list that holds a row of the call, its first row and their number; false for rows behind the last entry's.
-__device__ __forceinline__ bool entry_of_row(const PageRows& r, int row, int* i, int* first, int* m) {
-  *i = row;
-  if (r.row_off) {
-    int lo = 0, hi = r.n;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (r.row_off[mid] <= row) lo = mid; else hi = mid;
-    }
-    *i = lo;
+// Consecutive rows of an entry; n_rows: rows times pack (query heads that share a tile); pos0: position of the first row.
+struct RowsTile {
+  int row0, n_rows, pos0, seq;
+};
+
+// A lane's entry of a group of 32: its first row, rows, tiles of ROWS, sequence and length.
+template <int ROWS> struct RowsEntries {
+  int first = 0, m = 0, tiles = 0, seq = -1, len = 0, group = -1;
+
+  __device__ __forceinline__ void look_up(const PageView& pv, const PageRows& rows, int pack, int i0) {
+    if (i0 == group) return;
+    group = i0; first = m = tiles = len = 0; seq = -1;
+    const int i = i0 + (int)(threadIdx.x & 31);
+    if (i >= rows.n) return;
+    seq = page_seq_of(pv, rows.seqs, i);
+    page_rows_of(rows, i, &first, &m);
+    if (seq >= 0) len = page_len_of(pv, seq);
+    tiles = m > rows.max_rows ? 0 : (int)(((long long)m * pack + ROWS - 1) / ROWS);
   }
-  page_rows_of(r, *i, first, m);
-  return row >= *first && row < *first + *m;
-}
+  // Tile `slot` of all entries' (whole warp): false if there is none.
+  __device__ __forceinline__ bool find(const PageView& pv, const PageRows& rows, int pack, int slot, RowsTile& it) {
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int i0 = 0; i0 < rows.n; i0 += 32) {
+      look_up(pv, rows, pack, i0);
+      int incl = tiles;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      const int at = before + incl - tiles;
+      const uint32_t here = __ballot_sync(0xffffffffu, slot >= at && slot < at + tiles);
+      if (here) {
+        const int src = __ffs(here) - 1;
+        const int skip = (slot - __shfl_sync(0xffffffffu, at, src)) * ROWS, rows_here = __shfl_sync(0xffffffffu, m, src);
+        it.row0 = __shfl_sync(0xffffffffu, first, src) + skip;
+        it.n_rows = min(ROWS, (rows_here - skip) * pack);   // (pack > 1: one item, skip is 0)
+        it.pos0 = __shfl_sync(0xffffffffu, len, src) - rows_here + skip;
+        it.seq = __shfl_sync(0xffffffffu, seq, src);
+        return true;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    return false;
+  }
+};
 
 // HD / 32 consecutive elements of a row per lane, as floats.
 template <typename T, int N> __device__ __forceinline__ void load_dims(const T* p, float (&v)[N]);

@@ -90,8 +90,8 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&u)[16]) {
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 
 // What a CTA works on next, worked out by the producer warp and published two items ahead.
-struct RowsItem {
-  int head, row0, n_rows, pos0, seq;   // head (of the heads / pack) -1: there is nothing left; n_rows: rows times pack; pos0: position of the first row
+struct RowsItem : RowsTile {
+  int head;   // of the heads / pack; -1: there is nothing left
   // The keys as a list of boxes: 0 .. sink_boxes - 1 hold sinks, those from `first` on are box b + skew of the sequence, and the
   // places between them are left empty.
   int n_chunks, sink_boxes, skew, first;
@@ -163,49 +163,6 @@ __device__ __forceinline__ bool cut_keys(RowsItem& r, int split, int w) {
   }
   return true;
 }
-
-// A lane's entry of a group of 32: its first row, rows, pairs of tiles, sequence and length.
-struct RowsEntries {
-  int first = 0, m = 0, pairs = 0, seq = -1, len = 0, group = -1;
-
-  __device__ __forceinline__ void look_up(const PageView& pv, const PageRows& rows, int pack, int i0) {
-    if (i0 == group) return;
-    group = i0; first = m = pairs = len = 0; seq = -1;
-    const int i = i0 + (int)(threadIdx.x & 31);
-    if (i >= rows.n) return;
-    seq = page_seq_of(pv, rows.seqs, i);
-    page_rows_of(rows, i, &first, &m);
-    if (seq >= 0) len = page_len_of(pv, seq);
-    pairs = m > rows.max_rows ? 0 : (int)(((long long)m * pack + RW_ROWS - 1) / RW_ROWS);
-  }
-  // The item of pair `slot` of all entries' (whole warp): false if there is none.
-  __device__ __forceinline__ bool find(const PageView& pv, const PageRows& rows, int pack, int slot, RowsItem& it) {
-    const int lane = threadIdx.x & 31;
-    int before = 0;
-    for (int i0 = 0; i0 < rows.n; i0 += 32) {
-      look_up(pv, rows, pack, i0);
-      int incl = pairs;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
-      }
-      const int at = before + incl - pairs;
-      const uint32_t here = __ballot_sync(0xffffffffu, slot >= at && slot < at + pairs);
-      if (here) {
-        const int src = __ffs(here) - 1;
-        const int skip = (slot - __shfl_sync(0xffffffffu, at, src)) * RW_ROWS, rows_here = __shfl_sync(0xffffffffu, m, src);
-        it.row0 = __shfl_sync(0xffffffffu, first, src) + skip;
-        it.n_rows = min(RW_ROWS, (rows_here - skip) * pack);   // (pack > 1: one item, skip is 0)
-        it.pos0 = __shfl_sync(0xffffffffu, len, src) - rows_here + skip;
-        it.seq = __shfl_sync(0xffffffffu, seq, src);
-        return true;
-      }
-      before += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    return false;
-  }
-};
 
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   uint64_t r;
@@ -293,11 +250,11 @@ __global__ void __launch_bounds__(RW_THREADS, 1)
     if (warp == 0) {
       // ===================== producer: what comes next, and K and V by TMA (lane = (box, half) of the chunk) =====================
       const int n = p.rows.n;
-      RowsEntries e;
+      RowsEntries<RW_ROWS> e;
       int total = 0;   // pairs of tiles of all entries
       for (int i0 = 0; i0 < n; i0 += 32) {
         e.look_up(pv, p.rows, pack, i0);
-        total += __reduce_add_sync(0xffffffffu, e.pairs);
+        total += __reduce_add_sync(0xffffffffu, e.tiles);
         if (blockIdx.x == 0 && (e.m > p.rows.max_rows || (e.m > 0 && e.seq < 0))) atomicOr(pv.status, DEV_ERR_INDEX_RANGE);   // cannot be answered
       }
       const int split = SPLIT ? split_of((long long)total * heads, p.grid) : 1;
@@ -737,11 +694,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) rows_join_kernel(const RowsParam
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const PageView& pv = p.pv;
   const int window = p.a.window, sinks = p.a.sinks, pack = p.pack, heads = p.a.heads / pack;
-  RowsEntries e;
+  RowsEntries<RW_ROWS> e;
   int total = 0;
   for (int i0 = 0; i0 < p.rows.n; i0 += 32) {
     e.look_up(pv, p.rows, pack, i0);
-    total += __reduce_add_sync(0xffffffffu, e.pairs);
+    total += __reduce_add_sync(0xffffffffu, e.tiles);
   }
   RowsItem it{};
   if ((long long)blockIdx.x < (long long)total * heads && e.find(pv, p.rows, pack, total - 1 - (int)(blockIdx.x / heads), it))

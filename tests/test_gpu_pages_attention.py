@@ -431,3 +431,26 @@ def test_few_rows_of_grouped_heads_beside_what_they_must_not_touch():
     assert torch.isnan(out[7:9, 8:16]).all()
     compare(out[:5, 8:16], None, q[:5], keys[:1], values[:1], lens[:1], [5], 0, 0)
     compare(out[5:7, 8:16], None, q[5:7], [keys[1][:298]], [values[1][:298]], [298], [2], 0, 0)
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 0), (200, 9), (33, 200)])
+def test_rows_of_the_fp32_configuration(head_dim, page, window, sinks):
+    """Tiles of 32 rows that end inside an entry, entries of no rows, clusters that share chunks and tiles of a single one."""
+    run([1000, 40, 7, 0, 333], [70, 40, 3, 0, 32], 4, 2, head_dim, page, "fp32", window=window, sinks=sinks)
+    run([2100], [33], 2, 1, head_dim, page, "fp32", window=window, sinks=sinks)
+    run([600] * 20, [65] * 20, 8, 8, head_dim, page, "fp32", window=window, sinks=sinks)
+
+
+def test_a_page_that_is_missing_for_rows_of_the_fp32_configuration():
+    cache, table, q, keys, values = build([400, 400], [50, 50], 4, 2, 64, 16, "fp32")
+    kw = dict(row_off=dev(np.array([0, 50, 100])), max_rows=50)
+    want = cache.attention(0, q, **kw)
+    cache.poll()
+    cache.page_table[0, 3] = 1 << 20
+    got = cache.attention(0, q, **kw)
+    with pytest.raises(binding.RdError) as e:
+        cache.poll()
+    assert e.value.code == 1
+    assert torch.equal(got[50:], want[50:])
