@@ -583,7 +583,7 @@ class PagedCache:
             raise ValueError(f"q: expected rows [n, heads, {self.head_dim}]")
         rows, heads = shape[0], shape[1]
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
         qp, qs = self._rows("q", q, shape)
         op, os_ = self._rows("out", out, shape)
         if lse is not None:
