@@ -235,8 +235,8 @@ int redrafter_pages_reset(rd_pages* h, void* stream) {
 
 int redrafter_pages_extend(rd_pages* h, const int32_t* seqs, const int32_t* n_new, int32_t n, void* stream) {
   if (int rc = enter_list(h, n)) return rc;
+  if (n == 0) return RD_OK;   // (an empty list may be null)
   if (!n_new) return fail(h, RD_ERR_INVALID_ARG, "n_new is null");
-  if (n == 0) return RD_OK;
   int launches = 0;
   PCK(launch_pages_extend(h->pv, seqs, n_new, n, h->scratch, &launches, (cudaStream_t)stream));
   h->launches += launches;
@@ -245,8 +245,8 @@ int redrafter_pages_extend(rd_pages* h, const int32_t* seqs, const int32_t* n_ne
 
 int redrafter_pages_fork(rd_pages* h, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
   if (int rc = enter_list(h, n)) return rc;
-  if (!src || !dst) return fail(h, RD_ERR_INVALID_ARG, "null list");
   if (n == 0) return RD_OK;
+  if (!src || !dst) return fail(h, RD_ERR_INVALID_ARG, "null list");
   PCK(launch_pages_fork(h->pv, src, dst, n, (cudaStream_t)stream));
   h->launches++;
   return RD_OK;
@@ -255,9 +255,9 @@ int redrafter_pages_fork(rd_pages* h, const int32_t* src, const int32_t* dst, in
 int redrafter_pages_compact(rd_pages* h, const int32_t* seqs, const int32_t* n_rows, const int32_t* n_keep, const int32_t* rows,
                             int32_t row_stride, int32_t n, void* stream) {
   if (int rc = enter_list(h, n)) return rc;
+  if (n == 0) return RD_OK;
   if (!n_rows || !n_keep) return fail(h, RD_ERR_INVALID_ARG, "null list");
   if (rows && row_stride <= 0) return fail(h, RD_ERR_INVALID_ARG, "row_stride %d", row_stride);
-  if (n == 0) return RD_OK;
   int launches = 0;
   PCK(launch_pages_compact(h->pv, seqs, n_rows, n_keep, rows, row_stride, n, h->scratch, &launches, (cudaStream_t)stream));
   h->launches += launches;

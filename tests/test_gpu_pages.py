@@ -262,3 +262,27 @@ def test_on_another_stream():
         grow(cache, model, [5], [4], rng)
         model.check(cache)
         cache.poll()
+
+
+def test_empty_lists_change_nothing():
+    cache = binding.PagedCache.empty(2, 2, 64, 16, 8, 3, 4)
+    cache.extend(dev(np.array([5, 20, 0])))
+    before = [t.clone() for t in (cache.page_table, cache.lens, cache.refs, cache.free_bits)]
+    none = dev(np.zeros(0))
+    rows = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda:0")
+    launches = cache.launch_count()
+    cache.extend(none)
+    cache.extend(none, seqs=none)
+    cache.fork(none, none)
+    cache.compact(none, none, seqs=none)
+    cache.compact(none, none, rows=dev(np.zeros((0, 3))), seqs=none)
+    cache.trim(4, seqs=none)
+    cache.free(seqs=none)
+    cache.write(0, rows, rows, seqs=none)
+    cache.write(1, rows, rows, row_off=dev(np.zeros(1)))
+    assert cache.attention(0, rows, seqs=none).shape == (0, 2, 64)
+    assert cache.attention(0, rows, row_off=dev(np.zeros(3))).shape == (0, 2, 64)
+    cache.poll()
+    assert cache.launch_count() == launches
+    for a, b in zip(before, (cache.page_table, cache.lens, cache.refs, cache.free_bits)):
+        assert torch.equal(a, b)
