@@ -170,3 +170,18 @@ def test_refusals():
     with pytest.raises(RuntimeError):
         binding.token_logprobs(x.cpu(), t)
     assert binding.token_logprobs(x[:0], t[:0], top=3)["top_ids"].shape == (0, 3)
+
+
+def test_calls_on_two_streams_at_once():
+    logits = [torch.randn(300, 40000, device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(k)) for k in range(2)]
+    want = [binding.token_logprobs(x, top=8) for x in logits]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in logits]
+    for _ in range(5):
+        got = []
+        for stream, x in zip(streams, logits):
+            with torch.cuda.stream(stream):
+                got.append(binding.token_logprobs(x, top=8))
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(a[k], b[k]) for k in b)

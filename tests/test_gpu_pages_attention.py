@@ -454,3 +454,23 @@ def test_a_page_that_is_missing_for_rows_of_the_fp32_configuration():
         cache.poll()
     assert e.value.code == 1
     assert torch.equal(got[50:], want[50:])
+
+
+def test_handles_on_streams_of_their_own_at_once():
+    """Each handle's parts lie in its own workspace: calls on two streams do not meet."""
+    off = dev(np.array([0, 20, 21, 30]))
+    made = [build([3000, 1, 900], [20, 1, 9], 16, 4, 128, 32, dtype, seed=k) for k, dtype in enumerate(("bf16", "bf16", "fp32"))]
+    calls = [lambda c=c, q=q: (c.attention(0, q[:3]), c.attention(0, q, row_off=off, max_rows=20)) for c, _, q, _, _ in made]
+    want = [call() for call in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(10):
+        got = []
+        for stream, call in zip(streams, calls):
+            with torch.cuda.stream(stream):
+                got.append(call())
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    for c, *_ in made:
+        c.poll()
