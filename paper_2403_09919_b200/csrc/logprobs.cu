@@ -32,15 +32,16 @@ namespace cg = cooperative_groups;
 constexpr int LP_THREADS = 512, LP_WARPS = LP_THREADS / 32, LP_GROUPS = 128, LP_LIST = 2048;   // LP_GROUPS: most groups of threads
 typedef unsigned long long u64;
 
-// Order of the tokens as one number: larger logit first (NaN above all, as sorting puts it), lower index first.
+// Order of the tokens as one number: larger logit first (NaN above all, as sorting puts it), lower index first.  No key is ~0, which
+// stands above them all: +inf is 0xff800000 in the upper half, NaN 0xfffffffe.
 __device__ __forceinline__ u64 rank_key(float x, uint32_t index) {
   uint32_t u = __float_as_uint(x + 0.f);   // (-0 is 0)
-  u = x != x ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
+  u = x != x ? 0xfffffffeu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
   return ((u64)u << 32) | (0xffffffffu - index);
 }
 __device__ __forceinline__ float key_logit(u64 key) {
   const uint32_t u = (uint32_t)(key >> 32);
-  return __uint_as_float(u == 0xffffffffu ? 0x7fffffffu : (u & 0x80000000u) ? u & 0x7fffffffu : ~u);
+  return __uint_as_float(u == 0xfffffffeu ? 0x7fffffffu : (u & 0x80000000u) ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ uint32_t key_index(u64 key) { return 0xffffffffu - (uint32_t)key; }
 
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(LP_THREADS, sizeof(T) == 2 ? 3 : 0) logprob_ke
       rounds = s_count > LP_LIST;
     }
     if (rounds) {   // one maximum after another, each below the one before
-      u64 before = ~0ull;
+      u64 before = ~0ull;   // (above every key)
       for (int r = 0; r < a.top; ++r) {
         u64 m = 0;
         auto look = [&](float v, int index) {

@@ -185,3 +185,21 @@ def test_calls_on_two_streams_at_once():
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert all(torch.equal(a[k], b[k]) for k in b)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [9, 5000, 32000, 131072])
+def test_nan_in_the_first_place_and_everywhere(dtype, vocab):
+    """NaN stands above all, lowest id first, the first id among them too; all ids are ids of the vocabulary."""
+    top = min(vocab, 12)
+    x = torch.randn(5, vocab, generator=torch.Generator("cuda:0").manual_seed(vocab), device="cuda:0").to(dtype)
+    x[0, 0] = math.nan
+    x[1] = math.nan
+    x[2, 0], x[2, vocab - 1], x[2, 3] = math.nan, math.nan, math.inf
+    x[3, 0], x[3, 1:] = math.nan, -math.inf
+    x[4, 0] = math.inf
+    got = binding.token_logprobs(x, dev(np.zeros(5)), top=top)
+    want = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(got["top_ids"].long(), want)
+    for k in ("logprob", "entropy", "top_logprobs"):
+        assert torch.isnan(got[k]).all()
