@@ -474,7 +474,10 @@ RD_API int redrafter_use_pages(rd_handle* h, rd_pages* pages, const int32_t* seq
  * entropy and the `top` most likely tokens (see redrafter_token_logprobs).  Device buffers, each but the last two may be NULL:
  * logprob, entropy [B][L+1], top_ids, top_logprobs [B][L+1][top].  Column j of sequence b is its j-th emitted token: after
  * redrafter_step the accepted tokens and the bonus token, columns 0 .. n_accept[b]; after redrafter_ar_step and
- * redrafter_prefill (the root) column 0.  The other columns are NaN and -1.  Errors: STATE when the last call was none of these. */
+ * redrafter_prefill (the root) column 0.  The other columns are NaN and -1.  What was emitted is recorded on the device by the call's
+ * own launches: after a replay of a captured step it is the replay's.  A verification, an acceptance and redrafter_set_state end it.
+ * Errors: STATE when the last of these calls emitted nothing; on a handle of which an emitting call has been captured, whose
+ * replays the host does not see, all columns are NaN and -1 then. */
 RD_API int redrafter_last_logprobs(rd_handle* h, void* stream, int32_t top, float temperature, float* logprob, float* entropy, int32_t* top_ids,
                                    float* top_logprobs);
 

@@ -77,8 +77,6 @@ struct alignas(64) TensorMapBox {  // opaque storage of one CUtensorMap (128 byt
 enum { PROF_GEMM = 0, PROF_ATTN = 1, PROF_NORM = 2, PROF_ROPE = 3, PROF_SWIGLU = 4, PROF_DRAFT_SMALL = 5, PROF_PACK_ACCEPT = 6,
        PROF_MISC = 7, PROF_CLASSES = 8 };
 
-enum { EMITTED_NOTHING = 0, EMITTED_PROMPT = 1, EMITTED_AR = 2, EMITTED_STEP = 3 };   // the call that filled the logits
-
 struct rd_handle {
   rd_config cfg;
   Dims dm;
@@ -93,7 +91,8 @@ struct rd_handle {
   int ctx_bound;  // host-side upper bound of every sequence's context length
   int route_bound;  // the same without the feedback below: kernels are chosen by it, so that results follow from the calls alone
   Sampling sampling;  // how the LLM's tokens are chosen (inv_t = 0: greedy)
-  int emitted;    // what redrafter_last_logprobs is about: EMITTED_*
+  bool emitted = false;         // the last call that ran emitted tokens from the logits (what: on the device, EMITTED_*)
+  bool emits_captured = false;  // ... or a replay of one that was captured may have
   rd_pages* pages = nullptr;   // prompts and autoregressive steps run on them; nullptr: on the handle's own cache
   const int32_t* page_seqs = nullptr;
   int page_window = 0, page_sinks = 0;
@@ -453,6 +452,12 @@ bool capturing(cudaStream_t st) {
   cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
   if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) (void)cudaGetLastError();
   return cap != cudaStreamCaptureStatusNone;
+}
+
+// For redrafter_last_logprobs: a call that emits tokens (or does not, any more) is enqueued.  A captured one has not run.
+void note_emitted(rd_handle* h, cudaStream_t st, bool emits) {
+  if (!capturing(st)) h->emitted = emits;
+  else if (emits) h->emits_captured = true;
 }
 
 // Start of a chained region: counters back in step with the host if an earlier launch was counted but never ran.
@@ -984,7 +989,6 @@ int redrafter_init(const rd_config* cfg, const rd_weights* wt, void* kv_cache, s
     add_a(w.se_t, R, dm.dr + dm.d);
     if (!ok) return init_fail(h, RD_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d for operand %p", failed_rc, failed_ptr);
   }
-  h->emitted = EMITTED_NOTHING;
   h->prefilled = false; h->batch = dm.B; h->ctx_bound = h->route_bound = 0; h->launches = 0; h->err[0] = 0;
   for (int i = 0; i < RD_ROUTE_COUNT; ++i) h->route[i] = 0;
   h->sampling = Sampling{0.0f, 0u, 0u};
@@ -1087,7 +1091,7 @@ int redrafter_prefill(rd_handle* h, const int32_t* tokens, const int32_t* prompt
   // (the prompt would be baked into the graph, and a replay would leave the host's batch and bound as they are)
   if (capturing(st)) return fail(h, RD_ERR_STATE, "prompts cannot be processed under stream capture");
   if (int rc0 = check_pages(h, batch)) return rc0;
-  h->emitted = EMITTED_NOTHING;
+  h->emitted = false;
   h->batch = batch;
   int rc = set_row_counts(h, st);
   if (rc) return rc;
@@ -1137,11 +1141,12 @@ int redrafter_prefill(rd_handle* h, const int32_t* tokens, const int32_t* prompt
   rc = gemm(h, w.h_t, dm.d, h->w.lm_head, dm.V, dm.d, w.one_b, batch, w.logits, dm.V, &g, nullptr, st);
   if (rc) return rc;
   for (int i = 0; i < batch; i += PREFILL_TOKENS)
-    CK(h, launch_store_i32(w.ctx + i, prompt_len + i, batch - i < PREFILL_TOKENS ? batch - i : PREFILL_TOKENS, st));
+    CK(h, launch_store_i32(w.ctx + i, prompt_len + i, batch - i < PREFILL_TOKENS ? batch - i : PREFILL_TOKENS, w.m_total + 2,
+                           EMITTED_PROMPT | batch << EMITTED_BITS, st));
   // row b is sequence b's last prompt row: the root is the token at position prompt_len[b]
   CK(h, launch_argmax_rows(w.logits, g, dm.V, w.root, nullptr, w.one_b, batch, h->sampling, nullptr, w.ctx, 0, st));
   h->prefilled = true;
-  h->emitted = EMITTED_PROMPT;
+  h->emitted = true;
   h->ctx_bound = h->route_bound = longest;
   fb_invalidate(h);
   return RD_OK;
@@ -1171,7 +1176,7 @@ int redrafter_verify(rd_handle* h, const rd_packed* packed, void* stream, int32_
   int rc = check_stepable(h, (cudaStream_t)stream);
   if (rc) return rc;
   if (!packed_ok(packed) || !argmax) return fail(h, RD_ERR_INVALID_ARG, "null packed member or argmax");
-  h->emitted = EMITTED_NOTHING;
+  note_emitted(h, (cudaStream_t)stream, false);
   return do_verify(h, *packed, (cudaStream_t)stream, argmax, hidden, logits);
 }
 
@@ -1183,8 +1188,9 @@ int redrafter_accept(rd_handle* h, const int32_t* beams, const rd_packed* packed
   Workspace& w = h->ws;
   rd_accept_out o{};
   if (out) o = *out;
+  note_emitted(h, (cudaStream_t)stream, false);   // (accepted from the caller's rows, of which the logits here may know nothing)
   CK(h, launch_accept(h->dm.dtype, beams, *packed, argmax, hidden, nullptr, h->kv, w.ctx, w.root, w.h, o, w.n_accept, w.best,
-                      w.ctx_prev, h->dm, h->batch, w.status, (cudaStream_t)stream));
+                      w.ctx_prev, w.m_total + 2, EMITTED_NOTHING, h->dm, h->batch, w.status, (cudaStream_t)stream));
   h->launches++;  // accept + compaction
   fb_advance(h, 1 + h->dm.L, (cudaStream_t)stream);
   return RD_OK;
@@ -1207,8 +1213,9 @@ int redrafter_accept_static(rd_handle* h, const int32_t* beams, const rd_packed*
   Workspace& w = h->ws;
   rd_accept_out o{};
   if (out) o = *out;
+  note_emitted(h, (cudaStream_t)stream, false);
   CK(h, launch_accept(h->dm.dtype, beams, *packed, argmax, hidden, nullptr, h->kv, w.ctx, w.root, w.h, o, n_accept, best, ctx_prev,
-                      h->dm, h->batch, w.status, (cudaStream_t)stream));
+                      w.m_total + 2, EMITTED_NOTHING, h->dm, h->batch, w.status, (cudaStream_t)stream));
   h->launches++;  // accept + compaction
   fb_advance(h, 1 + h->dm.L, (cudaStream_t)stream);
   return RD_OK;
@@ -1219,7 +1226,7 @@ int redrafter_step(rd_handle* h, const int32_t* planted_beams, void* stream, con
   if (rc) return rc;
   cudaStream_t st = (cudaStream_t)stream;
   Workspace& w = h->ws;
-  h->emitted = EMITTED_NOTHING;
+  note_emitted(h, st, false);
   rc = do_draft(h, st, w.beams, w.scores);
   if (rc) return rc;
   const int32_t* beams = planted_beams ? planted_beams : w.beams;
@@ -1229,9 +1236,9 @@ int redrafter_step(rd_handle* h, const int32_t* planted_beams, void* stream, con
   rd_accept_out o{};
   if (out) o = *out;
   CKP(h, PROF_PACK_ACCEPT, launch_accept(h->dm.dtype, beams, w.pk, w.argmax_p, w.hidden_f, w.seq_off, h->kv, w.ctx, w.root, w.h, o, w.n_accept,
-                      w.best, w.ctx_prev, h->dm, h->batch, w.status, st));
+                      w.best, w.ctx_prev, w.m_total + 2, EMITTED_STEP | h->batch << EMITTED_BITS, h->dm, h->batch, w.status, st));
   h->launches++;
-  h->emitted = EMITTED_STEP;
+  note_emitted(h, st, true);
   fb_advance(h, 1 + h->dm.L, st);
   return RD_OK;
 }
@@ -1242,8 +1249,8 @@ int redrafter_ar_step(rd_handle* h, void* stream, int32_t* token) {
   fb_poll(h, (cudaStream_t)stream);
   if (h->ctx_bound + 1 > context_room(h)) return fail(h, RD_ERR_CAPACITY, "KV cache full");
   if (int rc0 = check_pages(h, h->batch)) return rc0;
-  h->emitted = EMITTED_NOTHING;
   cudaStream_t st = (cudaStream_t)stream;
+  note_emitted(h, st, false);
   Workspace& w = h->ws;
   const Dims& dm = h->dm;
   const int B = h->batch;
@@ -1255,8 +1262,8 @@ int redrafter_ar_step(rd_handle* h, void* stream, int32_t* token) {
   rc = gemm(h, w.hidden_t, dm.d, h->w.lm_head, dm.V, dm.d, w.m_total, B, w.logits, dm.V, &g, nullptr, st);
   if (rc) return rc;
   CK(h, launch_argmax_rows(w.logits, g, dm.V, w.argmax_c, nullptr, w.m_total, B, h->sampling, w.row_seq, w.row_pos, 1, st));
-  CK(h, launch_ar_finish(w.argmax_c, w.hidden_f, w.ctx, w.root, w.h, token, dm, B, st));
-  h->emitted = EMITTED_AR;
+  CK(h, launch_ar_finish(w.argmax_c, w.hidden_f, w.ctx, w.root, w.h, token, w.m_total + 2, dm, B, st));
+  note_emitted(h, st, true);
   fb_advance(h, 1, st);
   return RD_OK;
 }
@@ -1282,7 +1289,7 @@ int redrafter_use_pages(rd_handle* h, rd_pages* pages, const int32_t* seqs, int3
 
 int redrafter_last_logprobs(rd_handle* h, void* stream, int32_t top, float temperature, float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs) {
   if (!h) return RD_ERR_INVALID_ARG;
-  if (h->emitted == EMITTED_NOTHING) return fail(h, RD_ERR_STATE, "no prompt, step or autoregressive step has filled the logits last");
+  if (!h->emitted && !h->emits_captured) return fail(h, RD_ERR_STATE, "no prompt, step or autoregressive step has filled the logits last");
   const Dims& dm = h->dm;
   Workspace& w = h->ws;
   if (top < 0 || top > LOGPROB_MAX_TOP || top > dm.V) return fail(h, RD_ERR_SHAPE, "top %d (at most %d)", top, LOGPROB_MAX_TOP);
@@ -1290,8 +1297,7 @@ int redrafter_last_logprobs(rd_handle* h, void* stream, int32_t top, float tempe
   if (top && (!top_ids || !top_logprobs)) return fail(h, RD_ERR_INVALID_ARG, "top_ids or top_logprobs is null");
   cudaStream_t st = (cudaStream_t)stream;
   const int B = h->batch;
-  const EmittedRows e{B, dm.L, dm.NMAX, h->emitted == EMITTED_PROMPT ? w.root : h->emitted == EMITTED_AR ? w.argmax_c : nullptr,
-                      w.n_accept, w.best, w.pk.unpack, w.seq_off, w.argmax_p};
+  const EmittedRows e{B, dm.L, dm.NMAX, w.m_total + 2, w.root, w.argmax_c, w.n_accept, w.best, w.pk.unpack, w.seq_off, w.argmax_p};
   CK(h, launch_emitted_rows(e, dm.BW, w.emit_row, w.emit_tok, st));
   LogprobArgs a{};
   a.logits = w.logits; a.row_stride = dm.V; a.row_index = w.emit_row; a.tokens = w.emit_tok; a.rows = B * (dm.L + 1); a.vocab = dm.V;
@@ -1326,9 +1332,10 @@ int redrafter_set_state(rd_handle* h, void* stream, const int32_t* ctx, const in
   if (batch <= 0 || batch > h->dm.B) return fail(h, RD_ERR_INVALID_ARG, "batch %d outside [1, %d]", batch, h->dm.B);
   cudaStream_t st = (cudaStream_t)stream;
   h->batch = batch;
-  h->emitted = EMITTED_NOTHING;
+  note_emitted(h, st, false);
   int rc = set_row_counts(h, st);
   if (rc) return rc;
+  CKRT(h, cudaMemsetAsync(h->ws.m_total + 2, 0, sizeof(int32_t), st));   // EMITTED_NOTHING
   const size_t B = batch;
   if (ctx) {
     CKRT(h, cudaMemcpyAsync(h->ws.ctx, ctx, B * sizeof(int32_t), cudaMemcpyDeviceToDevice, st));

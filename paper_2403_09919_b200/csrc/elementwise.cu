@@ -1054,7 +1054,7 @@ __global__ void __launch_bounds__(1024) build_rows_tree_kernel(rd_packed pk, con
     for (int k = 0; k < w; ++k) before += warp_tot[k];
     if (b < B) off[b] = before + incl - n;
     for (int k = 0; k < 32; ++k) acc += warp_tot[k];
-    if (threadIdx.x == 0 && b0 + (int)blockDim.x >= B) { off[B] = acc; *m_total = acc; }
+    if (threadIdx.x == 0 && b0 + (int)blockDim.x >= B) { off[B] = acc; m_total[0] = acc; m_total[2] = EMITTED_NOTHING; }
   }
   __syncthreads();
   for (int b = threadIdx.x; b <= B; b += blockDim.x) seq_off[b] = off[b];
@@ -1108,7 +1108,7 @@ __global__ void __launch_bounds__(256) build_rows_ar_kernel(const int32_t* __res
                                      Dims dm, int B, int* status) {
   pdl_enter();
   __shared__ int s_longest;
-  if (threadIdx.x == 0) { *m_total = B; seq_off[B] = B; s_longest = 0; }
+  if (threadIdx.x == 0) { m_total[0] = B; m_total[2] = EMITTED_NOTHING; seq_off[B] = B; s_longest = 0; }
   __syncthreads();
   for (int b = threadIdx.x; b < B; b += blockDim.x) {
     seq_off[b] = b;
@@ -1160,9 +1160,10 @@ __global__ void emitted_rows_kernel(EmittedRows e, int BW, int32_t* row, int32_t
   if (idx >= e.B * (e.L + 1)) return;
   const int b = idx / (e.L + 1), j = idx - b * (e.L + 1);
   int r = -1, t = -1;
-  if (e.tokens) {
-    if (j == 0) { r = b; t = e.tokens[b]; }
-  } else if (j <= e.n_accept[b]) {
+  const int kind = b < (*e.emitted >> EMITTED_BITS) ? *e.emitted & ((1 << EMITTED_BITS) - 1) : EMITTED_NOTHING;
+  if (kind == EMITTED_PROMPT || kind == EMITTED_AR) {
+    if (j == 0) { r = b; t = (kind == EMITTED_PROMPT ? e.root : e.argmax_c)[b]; }
+  } else if (kind == EMITTED_STEP && j <= e.n_accept[b]) {
     const int i = e.best[b], n = (unsigned)i < (unsigned)BW ? e.unpack[((size_t)b * BW + i) * (e.L + 1) + j] : -1;
     if ((unsigned)n < (unsigned)e.NMAX) { r = e.seq_off[b] + n; t = e.argmax[(size_t)b * e.NMAX + n]; }
   }
@@ -1177,7 +1178,7 @@ cudaError_t launch_emitted_rows(const EmittedRows& e, int BW, int32_t* row, int3
 
 // After an AR forward: ctx += 1, root = greedy token, h = hidden of the row.
 __global__ void ar_finish_kernel(const int32_t* __restrict__ argmax_c, const float* __restrict__ hidden_c, int32_t* ctx,
-                                 int32_t* root, float* h, int32_t* token_out, int d) {
+                                 int32_t* root, float* h, int32_t* token_out, int32_t* emitted, int d) {
   pdl_enter();
   const int b = blockIdx.x;
   for (int i = threadIdx.x; i < d; i += blockDim.x) h[(size_t)b * d + i] = hidden_c[(size_t)b * d + i];
@@ -1185,12 +1186,13 @@ __global__ void ar_finish_kernel(const int32_t* __restrict__ argmax_c, const flo
     ctx[b] += 1;
     root[b] = argmax_c[b];
     if (token_out) token_out[b] = argmax_c[b];
+    if (b == 0) *emitted = EMITTED_AR | (int)gridDim.x << EMITTED_BITS;
   }
 }
 
 cudaError_t launch_ar_finish(const int32_t* argmax_c, const float* hidden_c, int32_t* ctx, int32_t* root, float* h,
-                             int32_t* token_out, const Dims& dm, int B, cudaStream_t st) {
-  launch_pdl(ar_finish_kernel, B, 256, 0, st, argmax_c, hidden_c, ctx, root, h, token_out, dm.d);
+                             int32_t* token_out, int32_t* emitted, const Dims& dm, int B, cudaStream_t st) {
+  launch_pdl(ar_finish_kernel, B, 256, 0, st, argmax_c, hidden_c, ctx, root, h, token_out, emitted, dm.d);
   return cudaGetLastError();
 }
 
@@ -1226,7 +1228,7 @@ __global__ void __launch_bounds__(256) prefill_rows_kernel(const __grid_constant
         seq_off[b + 1] = b < p.b_first ? 0 : p.m;
         last_row[b] = -1;
       }
-    if (i0 == 0) { seq_off[0] = 0; m_total[0] = p.m; m_total[1] = p.longest; }
+    if (i0 == 0) { seq_off[0] = 0; m_total[0] = p.m; m_total[1] = p.longest; m_total[2] = EMITTED_NOTHING; }
   }
 }
 
@@ -1239,16 +1241,17 @@ cudaError_t launch_prefill_rows(const PrefillRows& p, int32_t* row_tok, int32_t*
 struct StoreI32 {
   int32_t v[PREFILL_TOKENS];
 };
-__global__ void __launch_bounds__(256) store_i32_kernel(const __grid_constant__ StoreI32 s, int32_t* dst, int n) {
+__global__ void __launch_bounds__(256) store_i32_kernel(const __grid_constant__ StoreI32 s, int32_t* dst, int n, int32_t* word, int32_t value) {
   pdl_enter();
+  if (threadIdx.x == 0) *word = value;
   for (int i = threadIdx.x; i < n; i += blockDim.x) dst[i] = s.v[i];
 }
 
-cudaError_t launch_store_i32(int32_t* dst, const int32_t* values, int n, cudaStream_t st) {
+cudaError_t launch_store_i32(int32_t* dst, const int32_t* values, int n, int32_t* word, int32_t value, cudaStream_t st) {
   if (n <= 0 || n > PREFILL_TOKENS) return cudaErrorInvalidValue;
   StoreI32 s;
   for (int i = 0; i < n; ++i) s.v[i] = values[i];
-  launch_pdl(store_i32_kernel, 1, 256, 0, st, s, dst, n);
+  launch_pdl(store_i32_kernel, 1, 256, 0, st, s, dst, n, word, value);
   return cudaGetLastError();
 }
 

@@ -111,8 +111,8 @@ __global__ void __launch_bounds__(256) accept_kernel(const int32_t* __restrict__
                                                       const int32_t* __restrict__ argmax, const float* __restrict__ hidden,
                                                       const int32_t* __restrict__ seq_off,
                                                       int32_t* ctx, int32_t* root, float* h, rd_accept_out out,
-                                                      int32_t* n_accept_ws, int32_t* best_ws, int32_t* ctx_prev, Dims dm,
-                                                      int* status) {
+                                                      int32_t* n_accept_ws, int32_t* best_ws, int32_t* ctx_prev,
+                                                      int32_t* emitted, int32_t emits, Dims dm, int* status) {
   pdl_enter();
   __shared__ int sh_a[8], sh_i[8];
   __shared__ int s_node, s_bonus;
@@ -178,6 +178,7 @@ __global__ void __launch_bounds__(256) accept_kernel(const int32_t* __restrict__
     ctx_prev[b] = c;
     ctx[b] = c + 1 + a;
     root[b] = s_bonus;
+    if (b == 0) *emitted = emits;
   }
   // hidden rows: padded [B][NMAX], or compact (sequence b's first row is seq_off[b])
   const float* src = hidden + (seq_off ? (size_t)seq_off[b] + s_node : rb + s_node) * dm.d;
@@ -230,13 +231,13 @@ __global__ void __launch_bounds__(256) compact_kv_kernel(char* __restrict__ kv, 
   }
 }
 
-// seq_off: hidden holds compact rows (sequence b's first at seq_off[b]); nullptr: padded [B][NMAX].
+// seq_off: hidden holds compact rows (sequence b's first at seq_off[b]); nullptr: padded [B][NMAX].  *emitted becomes emits.
 cudaError_t launch_accept(int dtype, const int32_t* beams, const rd_packed& pk, const int32_t* argmax,
                           const float* hidden, const int32_t* seq_off, void* kcache, int32_t* ctx, int32_t* root, float* h,
                           const rd_accept_out& out, int32_t* n_accept_ws, int32_t* best_ws, int32_t* ctx_prev,
-                          const Dims& dm, int B, int* status, cudaStream_t st) {
-  launch_pdl(accept_kernel, B, 256, 0, st, beams, pk, argmax, hidden, seq_off, ctx, root, h, out, n_accept_ws, best_ws, ctx_prev, dm,
-                                   status);
+                          int32_t* emitted, int32_t emits, const Dims& dm, int B, int* status, cudaStream_t st) {
+  launch_pdl(accept_kernel, B, 256, 0, st, beams, pk, argmax, hidden, seq_off, ctx, root, h, out, n_accept_ws, best_ws, ctx_prev, emitted,
+                                   emits, dm, status);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int es = dtype == RD_DTYPE_FP32 ? 4 : 2;

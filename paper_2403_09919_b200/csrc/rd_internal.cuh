@@ -39,7 +39,7 @@ struct RowTables {
   const int32_t* n_cache;     // [M] number of leading cache slots the row attends
   const int32_t* local;       // [M] index of the row inside its sequence's group of rows (its mask row)
   const uint32_t* mask;       // [B][NMAX][MW] tree mask or nullptr (causal: n_cache covers everything)
-  const int32_t* m_total;     // [2] number of valid rows, and the most keys that any of them attends (device)
+  const int32_t* m_total;     // [3] number of valid rows, the most keys that any of them attends, EMITTED_* (device)
 };
 
 struct Dims {
@@ -124,7 +124,8 @@ cudaError_t launch_page_growth(const int32_t* seq_off, const int32_t* row_pos, c
 // Row of the logits and token of everything that the last call emitted: [B][L + 1], -1 where nothing was.
 struct EmittedRows {
   int B, L, NMAX;
-  const int32_t* tokens;     // one token per sequence, its row of the logits the sequence's index; or nullptr: the last step's
+  const int32_t* emitted;            // EMITTED_* and the batch
+  const int32_t *root, *argmax_c;    // after a prompt, an autoregressive step: one token per sequence, its row of the logits the sequence's index
   const int32_t *n_accept, *best, *unpack, *seq_off, *argmax;
 };
 cudaError_t launch_emitted_rows(const EmittedRows& e, int BW, int32_t* row, int32_t* tok, cudaStream_t st);
@@ -188,6 +189,11 @@ cudaError_t launch_draft_select(int dtype, const GemmOut& proj, int call, float*
                                 int32_t* beams_out, float* scores_out, int32_t* counters, const int32_t* m_total,
                                 unsigned long long* dbg, const SelectScratch& sc, Chain* chain, cudaStream_t st);
 
+// What the call that wrote the logits last emitted, in a word on the device (Workspace::m_total[2]): one of these, and its batch
+// shifted by EMITTED_BITS.  The launches of every call that writes what emitted_rows_kernel reads set it, so that a replayed graph
+// does, too, of which the host learns nothing.
+enum { EMITTED_NOTHING = 0, EMITTED_PROMPT = 1, EMITTED_AR = 2, EMITTED_STEP = 3, EMITTED_BITS = 2 };
+
 // pack / accept
 cudaError_t launch_pack(const int32_t* beams, const int32_t* root, const int32_t* ctx, const rd_packed& out,
                         const Dims& dm, int B, int no_tree, cudaStream_t st);
@@ -212,7 +218,8 @@ struct PrefillRows {
 };
 cudaError_t launch_prefill_rows(const PrefillRows& p, int32_t* row_tok, int32_t* row_seq, int32_t* row_pos, int32_t* row_slot, int32_t* row_ncache,
                                 int32_t* row_local, int32_t* last_row, int32_t* seq_off, int32_t* m_total, cudaStream_t st);
-cudaError_t launch_store_i32(int32_t* dst, const int32_t* values, int n, cudaStream_t st);   // host values, n <= PREFILL_TOKENS
+// host values, n <= PREFILL_TOKENS; and *word = value
+cudaError_t launch_store_i32(int32_t* dst, const int32_t* values, int n, int32_t* word, int32_t value, cudaStream_t st);
 cudaError_t launch_scatter_rows(const float* src, int width, float* dst, const int32_t* row_out_index,
                                 const int32_t* m_total, int m_max, cudaStream_t st);
 cudaError_t launch_cast_rows(int dtype, const float* src, void* dst, int n, cudaStream_t st);
@@ -220,11 +227,11 @@ cudaError_t launch_fill_i32(int32_t* p, int32_t v, int n, cudaStream_t st);
 cudaError_t launch_accept(int dtype, const int32_t* beams, const rd_packed& pk, const int32_t* argmax,
                           const float* hidden, const int32_t* seq_off, void* kcache, int32_t* ctx, int32_t* root, float* h,
                           const rd_accept_out& out, int32_t* n_accept_ws, int32_t* best_ws, int32_t* ctx_prev,
-                          const Dims& dm, int B, int* status, cudaStream_t st);
+                          int32_t* emitted, int32_t emits, const Dims& dm, int B, int* status, cudaStream_t st);
 int accept_static_max_batch();
 cudaError_t accept_static_scratch(int32_t** n_accept, int32_t** best, int32_t** ctx_prev);
 cudaError_t launch_ar_finish(const int32_t* argmax_c, const float* hidden_c, int32_t* ctx, int32_t* root, float* h,
-                             int32_t* token_out, const Dims& dm, int B, cudaStream_t st);
+                             int32_t* token_out, int32_t* emitted, const Dims& dm, int B, cudaStream_t st);
 cudaError_t launch_prefill_finish(const float* hidden_c, const int32_t* last_row, float* h, int d, int B,
                                   cudaStream_t st);
 

@@ -295,3 +295,78 @@ def test_a_step_without_room_leaves_shared_pages_alone():
         r.eng.poll()
     assert torch.equal(cache.pool.view(torch.int16), before.view(torch.int16))
     assert cache.lens.tolist() == [20, 18]
+
+
+def same(a, b):
+    return all(torch.equal(torch.nan_to_num(a[k].float(), nan=7e9), torch.nan_to_num(b[k].float(), nan=7e9)) for k in a)
+
+
+@pytest.mark.parametrize("kind", ["step", "ar_step"])
+def test_log_probabilities_after_replays(kind):
+    """What a replayed graph emitted, whatever the host's last call was: a prompt, a verification."""
+    cfg = dict(synth.CONFIGS["tiny"], max_batch=2)
+    eager, rig = Rig(cfg=cfg), Rig(cfg=cfg)
+    rng = np.random.default_rng(12)
+    old, new = ([rng.integers(0, 1024, size=n) for n in lens] for lens in ((20, 31), (40, 9)))
+    out = [binding.AcceptOut(2, cfg["beam_length"], "cuda:0") for _ in range(2)]
+    token = [torch.zeros(2, dtype=torch.int32, device="cuda:0") for _ in range(2)]
+
+    def call(r, i):
+        r.eng.step(out=out[i]) if kind == "step" else r.eng.ar_step(token[i])
+
+    rig.eng.prefill(old)
+    call(rig, 0)
+    torch.cuda.synchronize()
+    before = rig.eng.last_logprobs(top=3)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(rig, 0)
+    assert same(before, rig.eng.last_logprobs(top=3))      # capturing has emitted nothing
+    rig.eng.prefill(new)
+    eager.eng.prefill(new)
+    assert same(rig.eng.last_logprobs(top=3), eager.eng.last_logprobs(top=3))
+    for _ in range(2):
+        g.replay()
+        call(eager, 1)
+        assert same(rig.eng.last_logprobs(top=3, temperature=0.9), eager.eng.last_logprobs(top=3, temperature=0.9))
+    rig.eng.set_ctx_bound(60)
+    beams, _ = rig.eng.draft()
+    rig.eng.verify(rig.eng.pack(beams))
+    nothing = rig.eng.last_logprobs(top=3)                 # (the host cannot know; the device does)
+    assert torch.isnan(nothing["logprob"]).all() and (nothing["top_ids"] == -1).all()
+    torch.cuda.synchronize()
+    del g
+
+
+def test_log_probabilities_of_a_graph_that_has_not_run():
+    """A captured step fills nothing."""
+    cfg = dict(synth.CONFIGS["tiny"], max_batch=2)
+    r = Rig(cfg=cfg)
+    r.eng.prefill([np.arange(20), np.arange(9)])
+    beams, _ = r.eng.draft()
+    r.eng.verify(r.eng.pack(beams))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.eng.step()
+    got = r.eng.last_logprobs(top=2)
+    assert torch.isnan(got["logprob"]).all() and torch.isnan(got["entropy"]).all() and (got["top_ids"] == -1).all()
+    torch.cuda.synchronize()
+    del g
+
+
+@pytest.mark.parametrize("accept", ["accept", "accept_static"])
+def test_log_probabilities_after_an_acceptance_of_the_callers(accept):
+    """The acceptance of rows that the caller verified leaves another root, and of accepted tokens the handle's logits know nothing."""
+    r = Rig(cfg=dict(synth.CONFIGS["tiny"], max_batch=2))
+    prompts = [np.arange(20), np.arange(9)]
+    r.eng.prefill(prompts)
+    beams, _ = r.eng.draft()
+    packed = r.eng.pack(beams)
+    argmax, hidden, _ = r.eng.verify(packed)
+    for before in (lambda: r.eng.prefill(prompts), r.eng.step, r.eng.ar_step):
+        before()
+        r.eng.last_logprobs()
+        getattr(r.eng, accept)(beams, packed, argmax, hidden)
+        with pytest.raises(binding.RdError) as e:
+            r.eng.last_logprobs()
+        assert e.value.code == 4
