@@ -462,7 +462,8 @@ RD_API const char* redrafter_token_logprobs_error(void);   /* why the last one f
  * room in `pages` (redrafter_pages_extend), write their K and V there and attend over it, with the window and sinks given
  * (0, 0: every earlier key); the handle's own cache is left alone.  Sequence b of the batch is row seqs[b] of the page table
  * (device [max_batch], borrowed; NULL: row b).  A prompt's sequences are empty before it; an autoregressive step's hold their
- * contexts (one that does not is reported by the next redrafter_poll).  Between calls the pages may be forked, trimmed and
+ * contexts (one that does not is reported by the next redrafter_poll and left out: its pages and its length in the table stay as they
+ * are, and what the pass computes of it is not defined).  Between calls the pages may be forked, trimmed and
  * freed, the state set to match (redrafter_set_state): sequences that share a prompt run it once.  Contexts are bounded by
  * max_seq_pages * page_size instead of max_ctx; too few free pages are reported by redrafter_pages_poll, and what the call that
  * met them computes is not defined.  Speculative calls (draft, pack, verify, accept, step) return STATE meanwhile.

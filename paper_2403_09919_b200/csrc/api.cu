@@ -678,7 +678,8 @@ int forward_layers(rd_handle* h, const uint32_t* mask, int m_max, int n_seq, int
   Chain* ch = paged ? nullptr : &h->chain;
   if (paged) {
     const PageView& pv = pages_view(h->pages);
-    CK(h, launch_page_growth(w.seq_off, w.row_pos, h->page_seqs, pv.lens, pv.max_seqs, n_seq, w.page_new, w.status, st));
+    const int prompt = after_w == nullptr;   // (its passes have no projection behind them)
+    CK(h, launch_page_growth(w.seq_off, w.row_pos, w.row_slot, h->page_seqs, pv.lens, pv.max_seqs, prompt, n_seq, w.page_new, w.status, st));
     int launches = 0;
     CKRT(h, pages_extend_for(h->pages, h->page_seqs, w.page_new, n_seq, &launches, st));
     h->launches += launches;

@@ -1137,19 +1137,25 @@ cudaError_t launch_build_rows_ar(const int32_t* root, const int32_t* ctx, int32_
   return cudaGetLastError();
 }
 
-__global__ void page_growth_kernel(const int32_t* __restrict__ seq_off, const int32_t* __restrict__ row_pos, const int32_t* __restrict__ seqs,
-                                   const int32_t* __restrict__ lens, int max_seqs, int B, int32_t* n_new, int32_t* status) {
+// A sequence whose pages hold another length than its context is left out: it does not grow, and its rows have no place to be written
+// (a later pass of its prompt might find its own first position there, so that what the pass before said of it counts).
+__global__ void page_growth_kernel(const int32_t* __restrict__ seq_off, const int32_t* __restrict__ row_pos, int32_t* row_slot, const int32_t* __restrict__ seqs,
+                                   const int32_t* __restrict__ lens, int max_seqs, int prompt, int B, int32_t* n_new, int32_t* status) {
   pdl_enter();
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b >= B) return;
-  const int m = seq_off[b + 1] - seq_off[b], s = seqs ? seqs[b] : b;
-  n_new[b] = m;
-  if (m > 0 && ((unsigned)s >= (unsigned)max_seqs || lens[s] != row_pos[seq_off[b]])) atomicOr(status, DEV_ERR_INDEX_RANGE);
+  const int first = seq_off[b], m = seq_off[b + 1] - first, s = seqs ? seqs[b] : b;
+  if (m <= 0) { n_new[b] = 0; return; }
+  const int pos = row_pos[first];
+  if ((unsigned)s < (unsigned)max_seqs && lens[s] == pos && !(prompt && pos > 0 && n_new[b] == 0)) { n_new[b] = m; return; }
+  atomicOr(status, DEV_ERR_INDEX_RANGE);
+  n_new[b] = 0;
+  for (int r = first; r < first + m; ++r) row_slot[r] = -1;
 }
 
-cudaError_t launch_page_growth(const int32_t* seq_off, const int32_t* row_pos, const int32_t* seqs, const int32_t* lens, int max_seqs, int B, int32_t* n_new,
-                               int32_t* status, cudaStream_t st) {
-  launch_pdl(page_growth_kernel, (B + 127) / 128, 128, 0, st, seq_off, row_pos, seqs, lens, max_seqs, B, n_new, status);
+cudaError_t launch_page_growth(const int32_t* seq_off, const int32_t* row_pos, int32_t* row_slot, const int32_t* seqs, const int32_t* lens, int max_seqs, int prompt, int B,
+                               int32_t* n_new, int32_t* status, cudaStream_t st) {
+  launch_pdl(page_growth_kernel, (B + 127) / 128, 128, 0, st, seq_off, row_pos, row_slot, seqs, lens, max_seqs, prompt, B, n_new, status);
   return cudaGetLastError();
 }
 

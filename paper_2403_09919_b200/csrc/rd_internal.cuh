@@ -117,10 +117,10 @@ struct KvPages {
 };
 cudaError_t launch_rope_kv(float* qkv, const GemmOut& proj, void* kcache, void* vcache, const float* table,
                            const RowTables& rt, const Dims& dm, int m_max, int* status, Chain* chain, const KvPages* pages, cudaStream_t st);
-// Rows of every sequence in the pass (from seq_off), for the pages to grow by; reports sequences whose pages do not hold their
-// context (row_pos of their first row).
-cudaError_t launch_page_growth(const int32_t* seq_off, const int32_t* row_pos, const int32_t* seqs, const int32_t* lens, int max_seqs, int B, int32_t* n_new,
-                               int32_t* status, cudaStream_t st);
+// Rows of every sequence in the pass (from seq_off), for the pages to grow by; sequences whose pages do not hold their context (row_pos
+// of their first row) are reported and left out.  prompt: a pass of prompts, whose n_new of the pass before is still there.
+cudaError_t launch_page_growth(const int32_t* seq_off, const int32_t* row_pos, int32_t* row_slot, const int32_t* seqs, const int32_t* lens, int max_seqs, int prompt, int B,
+                               int32_t* n_new, int32_t* status, cudaStream_t st);
 // Row of the logits and token of everything that the last call emitted: [B][L + 1], -1 where nothing was.
 struct EmittedRows {
   int B, L, NMAX;

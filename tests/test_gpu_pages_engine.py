@@ -370,3 +370,50 @@ def test_log_probabilities_after_an_acceptance_of_the_callers(accept):
         with pytest.raises(binding.RdError) as e:
             r.eng.last_logprobs()
         assert e.value.code == 4
+
+
+def test_pages_of_another_length_are_not_written():
+    """A prompt into a sequence that is not empty, a context shorter than its pages: reported, and the pages stay as they are; the
+    other sequences of the pass go on."""
+    r = Rig(cfg=CFG)
+    cache = pages_for(CFG, 16)
+    rng = np.random.default_rng(9)
+    r.eng.use_pages(cache, dev(np.array([1, 2, 3, 4])))
+    r.eng.prefill([rng.integers(0, CFG["vocab"], size=n) for n in (50, 23)])
+    r.eng.poll()
+    before = [t.clone() for t in (cache.pool.view(torch.int16), cache.page_table, cache.refs)]
+
+    def unchanged(lens):
+        with pytest.raises(binding.RdError) as e:
+            r.eng.poll()
+        assert e.value.code == 1
+        cache.poll()
+        assert cache.lens.tolist() == lens
+        table = cache.page_table.tolist()
+        held = [p for s in (1, 2) for p in table[s] if p >= 0]
+        assert [t[:5] for t in table[1:3]] == [t[:5] for t in before[1].tolist()[1:3]]
+        assert torch.equal(cache.pool.view(torch.int16)[:, :, held], before[0][:, :, held])
+
+    r.eng.prefill([rng.integers(0, CFG["vocab"], size=n) for n in (20, 64, 30)])       # sequences 1 and 2 are not empty, 3 is
+    unchanged([0, 50, 23, 30, 0, 0, 0, 0])
+    r.eng.set_state(dev(np.array([30, 22, 30])), dev(np.array([1, 2, 3])), None, batch=3, ctx_bound=50)
+    r.eng.ar_step()
+    unchanged([0, 50, 23, 31, 0, 0, 0, 0])
+
+
+def test_a_later_pass_of_a_prompt_that_was_left_out():
+    """A prompt of several passes into a sequence that holds as many tokens as the first pass takes: all of it is left out."""
+    cfg = dict(CFG, max_batch=1, max_ctx=2700)
+    r = Rig(cfg=cfg)
+    cache = pages_for(cfg, 64, n_pages=50, max_seqs=2, max_pages=45)
+    rng = np.random.default_rng(10)
+    r.eng.use_pages(cache)
+    r.eng.prefill([rng.integers(0, cfg["vocab"], size=1024)])
+    r.eng.poll()
+    before = cache.pool.clone()
+    r.eng.prefill([rng.integers(0, cfg["vocab"], size=1500)])
+    with pytest.raises(binding.RdError):
+        r.eng.poll()
+    cache.poll()
+    assert cache.lens.tolist() == [1024, 0]
+    assert torch.equal(cache.pool.view(torch.int16), before.view(torch.int16))
