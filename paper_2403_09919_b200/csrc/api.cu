@@ -95,6 +95,7 @@ struct rd_handle {
   bool emits_captured = false;  // ... or a replay of one that was captured may have
   rd_pages* pages = nullptr;   // prompts and autoregressive steps run on them; nullptr: on the handle's own cache
   const int32_t* page_seqs = nullptr;
+  bool ctx_in_pages = false;   // the contexts are those of what ran on pages: the handle's own cache does not hold them
   int page_window = 0, page_sinks = 0;
   int64_t launches;
   int64_t route[RD_ROUTE_COUNT];  // launches per kernel variant (redrafter_route_counts)
@@ -764,6 +765,13 @@ int forward_layers(rd_handle* h, const uint32_t* mask, int m_max, int n_seq, int
   return RD_OK;
 }
 
+// Whether there are contexts to go on from in the cache in use.
+int check_state(rd_handle* h) {
+  if (!h->prefilled) return fail(h, RD_ERR_STATE, "no state: call redrafter_prefill or redrafter_set_state first");
+  if (!h->pages && h->ctx_in_pages) return fail(h, RD_ERR_STATE, "the contexts lie in pages: call redrafter_prefill or pass contexts of the handle's own cache to redrafter_set_state first");
+  return RD_OK;
+}
+
 // Tokens that a sequence can hold.
 long long context_room(const rd_handle* h) {
   if (!h->pages) return h->dm.max_ctx;
@@ -774,7 +782,7 @@ long long context_room(const rd_handle* h) {
 int check_stepable(rd_handle* h, cudaStream_t st) {
   if (!h) return RD_ERR_INVALID_ARG;
   if (h->pages) return fail(h, RD_ERR_STATE, "pages are in use: speculative steps run on the handle's own cache");
-  if (!h->prefilled) return fail(h, RD_ERR_STATE, "no state: call redrafter_prefill or redrafter_set_state first");
+  if (int rc0 = check_state(h)) return rc0;
   fb_poll(h, st);
   if (h->ctx_bound + h->dm.NMAX > h->dm.max_ctx)
     return fail(h, RD_ERR_CAPACITY, "context bound %d + %d packed rows exceeds max_ctx %d", h->ctx_bound, h->dm.NMAX,
@@ -1092,6 +1100,7 @@ int redrafter_prefill(rd_handle* h, const int32_t* tokens, const int32_t* prompt
   // (the prompt would be baked into the graph, and a replay would leave the host's batch and bound as they are)
   if (capturing(st)) return fail(h, RD_ERR_STATE, "prompts cannot be processed under stream capture");
   if (int rc0 = check_pages(h, batch)) return rc0;
+  h->ctx_in_pages = h->pages != nullptr;
   h->emitted = false;
   h->batch = batch;
   int rc = set_row_counts(h, st);
@@ -1246,10 +1255,11 @@ int redrafter_step(rd_handle* h, const int32_t* planted_beams, void* stream, con
 
 int redrafter_ar_step(rd_handle* h, void* stream, int32_t* token) {
   if (!h) return RD_ERR_INVALID_ARG;
-  if (!h->prefilled) return fail(h, RD_ERR_STATE, "no state: call redrafter_prefill or redrafter_set_state first");
+  if (int rc0 = check_state(h)) return rc0;
   fb_poll(h, (cudaStream_t)stream);
   if (h->ctx_bound + 1 > context_room(h)) return fail(h, RD_ERR_CAPACITY, "KV cache full");
   if (int rc0 = check_pages(h, h->batch)) return rc0;
+  if (h->pages) h->ctx_in_pages = true;
   cudaStream_t st = (cudaStream_t)stream;
   note_emitted(h, st, false);
   Workspace& w = h->ws;
@@ -1341,6 +1351,7 @@ int redrafter_set_state(rd_handle* h, void* stream, const int32_t* ctx, const in
   if (ctx) {
     CKRT(h, cudaMemcpyAsync(h->ws.ctx, ctx, B * sizeof(int32_t), cudaMemcpyDeviceToDevice, st));
     fb_invalidate(h);   // copies of the old context lengths say nothing about the new ones
+    h->ctx_in_pages = false;
   }
   if (root) CKRT(h, cudaMemcpyAsync(h->ws.root, root, B * sizeof(int32_t), cudaMemcpyDeviceToDevice, st));
   if (hvec) CKRT(h, cudaMemcpyAsync(h->ws.h, hvec, B * h->dm.d * sizeof(float), cudaMemcpyDeviceToDevice, st));

@@ -417,3 +417,38 @@ def test_a_later_pass_of_a_prompt_that_was_left_out():
     cache.poll()
     assert cache.lens.tolist() == [1024, 0]
     assert torch.equal(cache.pool.view(torch.int16), before.view(torch.int16))
+
+
+def test_contexts_that_lie_in_pages_are_not_taken_for_the_handles_own():
+    """Back on the handle's own cache, which holds nothing of what ran on pages: refused until a prompt or a state says otherwise."""
+    r = Rig(cfg=CFG)
+    cache = pages_for(CFG, 16)
+    prompt = np.arange(40)
+
+    def refused(call):
+        with pytest.raises(binding.RdError) as e:
+            call()
+        assert e.value.code == 4
+
+    r.eng.prefill([prompt])
+    own = r.eng.get_state()
+    r.eng.use_pages(cache)
+    r.eng.prefill([prompt])
+    r.eng.use_pages(None)
+    for call in (r.eng.step, r.eng.ar_step, r.eng.draft):
+        refused(call)
+    r.eng.use_pages(cache)
+    r.eng.ar_step()                                   # the pages still hold it
+    r.eng.use_pages(None)
+    refused(r.eng.step)
+    r.eng.set_state(None, own[1], None)               # (no contexts: those of the pages)
+    refused(r.eng.step)
+    r.eng.set_state(*own, ctx_bound=40)               # what the handle's own cache held before
+    r.eng.step()
+    r.eng.poll()
+    cache.poll()
+    r.eng.prefill([prompt])
+    r.eng.use_pages(cache)                            # pages in use and not yet run on change nothing
+    r.eng.use_pages(None)
+    r.eng.step()
+    r.eng.poll()
