@@ -212,6 +212,12 @@ class AcceptOut:
         self.c = RdAcceptOut(self.n_accept.data_ptr(), self.best.data_ptr(), self.tokens.data_ptr())
 
 
+def _check_open(cache):
+    """A closed PagedCache has no handle behind it any more."""
+    if cache is not None and cache.h is None:
+        raise ValueError("the PagedCache has been closed")
+
+
 class ReDrafter:
     """A handle plus the device buffers it borrows (KV cache, workspace), allocated with torch."""
 
@@ -255,6 +261,7 @@ class ReDrafter:
         if rc:
             raise RdError(rc, "redrafter_init failed: " + self.L.redrafter_last_error(None).decode())
         self.h = hp
+        self._pages = (None, None)
         self.B = cfg["max_batch"]
         self.BW, self.Lb, self.d, self.V = cfg["beam_width"], cfg["beam_length"], cfg["d_model"], cfg["vocab"]
         self.nmax = 1 + self.BW * self.Lb
@@ -285,6 +292,7 @@ class ReDrafter:
         for b, p in enumerate(prompts):
             tok[b, :len(p)] = np.asarray(p, dtype=np.int32)
             ln[b] = len(p)
+        _check_open(self._pages[0])
         self.B = B
         self._ck(self.L.redrafter_prefill(self.h, tok.ctypes.data, ln.ctypes.data, mp, B, _stream()))
 
@@ -324,6 +332,7 @@ class ReDrafter:
         return out
 
     def ar_step(self, token=None):
+        _check_open(self._pages[0])
         self._ck(self.L.redrafter_ar_step(self.h, _stream(), _ptr(token)))
         return token
 
@@ -354,6 +363,7 @@ class ReDrafter:
         if seqs is not None and (seqs.dtype != torch.int32 or seqs.device != self.device or not seqs.is_contiguous() or
                                  seqs.numel() != self.cfg["max_batch"]):
             raise ValueError(f"seqs: expected {self.cfg['max_batch']} contiguous int32 on {self.device}")
+        _check_open(cache)
         self._ck(self.L.redrafter_use_pages(self.h, cache.h if cache is not None else None, _ptr(seqs), int(window), int(sinks)))
         self._pages = (cache, seqs)                 # keep them alive
 

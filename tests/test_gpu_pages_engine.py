@@ -452,3 +452,21 @@ def test_contexts_that_lie_in_pages_are_not_taken_for_the_handles_own():
     r.eng.use_pages(None)
     r.eng.step()
     r.eng.poll()
+
+
+def test_a_closed_cache_is_refused():
+    r = Rig(cfg=CFG)
+    cache = pages_for(CFG, 16)
+    r.eng.use_pages(cache)
+    r.eng.prefill([np.arange(10)])
+    torch.cuda.synchronize()
+    cache.close()
+    for call in (lambda: r.eng.prefill([np.arange(10)]), r.eng.ar_step, lambda: r.eng.use_pages(cache)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(binding.RdError):
+        cache.reset()
+    r.eng.use_pages(None)
+    r.eng.prefill([np.arange(10)])
+    r.eng.step()
+    r.eng.poll()
