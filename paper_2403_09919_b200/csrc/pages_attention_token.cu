@@ -11,8 +11,10 @@
 //   - A producer warp copies chunks by TMA, a page's rows at a time, into a ring of six stages of 32 KB that runs ahead over
 //     the ends of items: while a part is joined and written, the stream goes on.
 //   - Four warps take 16 keys of every chunk each, on their own: scores by mma (16 query rows; a single token has few rows,
-//     so the tensor cores are nowhere near their rate), running maximum and sum per row, weights to bf16, V by ldmatrix.trans.
-//     What they hold is joined in shared memory at the end of an item.
+//     so the tensor cores are nowhere near their rate), running maximum and sum per row, V by ldmatrix.trans.  Weights go in two
+//     bf16 parts, as in attention_kl.cu, which serves single tokens on the contiguous cache; the second takes the tile's rows 8 to 15
+//     where up to 8 query heads leave them free, and products of its own beyond.
+//     What the warps hold is joined in shared memory at the end of an item.
 //   - An item that crosses CTAs leaves its parts (unscaled output, maximum, sum, fp32) in the workspace; the last CTA to
 //     arrive joins them in the order of the CTAs, so that the result does not depend on who is last.
 // Measured with the write of the tokens' K and V before it (a launch of its own, 4 us of these): 16 sequences, 296 MB of K and V,
@@ -344,6 +346,13 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// Two weights in two bf16 parts each: the leading bits, cut off, and what is left, rounded (off by 2^-16 of the weight at most; one
+// part alone 2^-8).  The last bit is set first, so that what is left is never zero: 0 times an infinite V would not be infinite.
+__device__ __forceinline__ void split_bf16(float x, float y, uint32_t* high, uint32_t* low) {
+  const uint32_t a = __float_as_uint(x) | 1u, b = __float_as_uint(y) | 1u;
+  *high = __byte_perm(a, b, 0x7632);
+  *low = pack_bf16(__uint_as_float(a) - __uint_as_float(a & 0xffff0000u), __uint_as_float(b) - __uint_as_float(b & 0xffff0000u));
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
@@ -488,7 +497,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
           if (!(w & 256u)) c1[0] = c1[2] = -INFINITY;
           if (!(w & 512u)) c1[1] = c1[3] = -INFINITY;
         }
-        uint32_t pa[4];
+        uint32_t pa[4], pb[4];   // the weights in two parts
 #pragma unroll
         for (int r = 0; r < (WIDE ? 2 : 1); ++r) {
           float mx = fmaxf(fmaxf(c0[2 * r], c0[2 * r + 1]), fmaxf(c1[2 * r], c1[2 * r + 1]));
@@ -500,15 +509,18 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
             const float corr = fast_exp2(m[r] - ref);
             l[r] *= corr;
 #pragma unroll
-            for (int d = 0; d < HD / 8; ++d) { o[d][2 * r] *= corr; o[d][2 * r + 1] *= corr; }
+            for (int d = 0; d < HD / 8; ++d) {
+              o[d][2 * r] *= corr; o[d][2 * r + 1] *= corr;
+              if (!WIDE) { o[d][2] *= corr; o[d][3] *= corr; }
+            }
             m[r] = m_new;
           }
           const float p0 = fast_exp2(fmaf(c0[2 * r], scale2, -ref)), p1 = fast_exp2(fmaf(c0[2 * r + 1], scale2, -ref));
           const float p2 = fast_exp2(fmaf(c1[2 * r], scale2, -ref)), p3 = fast_exp2(fmaf(c1[2 * r + 1], scale2, -ref));
           l[r] += (p0 + p1) + (p2 + p3);
-          pa[r] = pack_bf16(p0, p1); pa[r + 2] = pack_bf16(p2, p3);   // (the weights' rounding: half a step of bf16 each, as in the library's other kernels)
+          split_bf16(p0, p1, &pa[r], &pb[r]); split_bf16(p2, p3, &pa[r + 2], &pb[r + 2]);
         }
-        if (!WIDE) pa[1] = pa[3] = 0u;
+        if (!WIDE) { pa[1] = pb[0]; pa[3] = pb[2]; }   // (rows 8 to 15 of the tile are free)
         const uint32_t z0 = ((seen >> (2 * t4)) & 1u ? 0xffffu : 0u) | ((seen >> (2 * t4 + 1)) & 1u ? 0xffff0000u : 0u);
         const uint32_t z1 = ((seen >> (2 * t4 + 8)) & 1u ? 0xffffu : 0u) | ((seen >> (2 * t4 + 9)) & 1u ? 0xffff0000u : 0u);
 #pragma unroll
@@ -519,6 +531,10 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
           if (seen != 0xffffu) { b[0] &= z0; b[1] &= z1; b[2] &= z0; b[3] &= z1; }
           mma_bf16(o[2 * d], pa, b[0], b[1]);
           mma_bf16(o[2 * d + 1], pa, b[2], b[3]);
+          if (WIDE) {
+            mma_bf16(o[2 * d], pb, b[0], b[1]);
+            mma_bf16(o[2 * d + 1], pb, b[2], b[3]);
+          }
         }
       }
       __syncwarp();
@@ -537,7 +553,7 @@ __global__ void __launch_bounds__(TK_THREADS, 1) pages_token_kernel(const __grid
       if (g + 8 * r < q_rows) {
         float* dst = s_out + (warp * 16 + g + 8 * r) * PITCH + 2 * t4;
 #pragma unroll
-        for (int d = 0; d < HD / 8; ++d) *reinterpret_cast<float2*>(dst + 8 * d) = make_float2(o[d][2 * r], o[d][2 * r + 1]);
+        for (int d = 0; d < HD / 8; ++d) *reinterpret_cast<float2*>(dst + 8 * d) = WIDE ? make_float2(o[d][2 * r], o[d][2 * r + 1]) : make_float2(o[d][0] + o[d][2], o[d][1] + o[d][3]);
       }
     }
     consumers_sync();

@@ -474,3 +474,39 @@ def test_handles_on_streams_of_their_own_at_once():
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
     for c, *_ in made:
         c.poll()
+
+
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(4, 4, 128), (32, 8, 128), (16, 1, 128), (40, 2, 64)])
+@pytest.mark.parametrize("window,sinks,qscale", [(0, 0, 1.0), (70, 5, 1.0), (0, 0, 4.0)])
+def test_single_tokens_weights_to_sixteen_bits(heads, kv_heads, head_dim, window, sinks, qscale):
+    """bf16: the weights that multiply V come in two parts, itself rounded to bf16 (off by 2^-8 of it at most) and what that left,
+    rounded again (2^-8 of that): 2^-16 of sum p |v| in place of 2^-8."""
+    lens = [1, 16, 17, 64, 63, 200, 129, 513, 2, 1000, 4000]
+    cache, table, q, keys, values = build(lens, [1] * len(lens), heads, kv_heads, head_dim, 32, "bf16", seed=heads, scale=qscale)
+    got = cache.attention(0, q, window=window, sinks=sinks)
+    cache.poll()
+    for i, n in enumerate(lens):
+        ref, _, absv, absqk = attend(q[i:i + 1], keys[i], values[i], np.array([n - 1]), window, sinks)
+        tol = tolerance(q.dtype, ref, absv, absqk, n, 1 / math.sqrt(head_dim)) - (2.0 ** -8 - 2.0 ** -16) * absv * (1 + 2.0 ** -8)
+        err = (got[i:i + 1].double() - ref).abs()
+        assert (err <= tol).all(), (n, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(4, 4), (16, 1)])
+def test_infinite_values_that_a_single_token_sees(heads, kv_heads):
+    """Weights of exactly one, of a few bits and of many: an infinity times any of them is infinite, in its own dimension alone."""
+    lens = [1, 2, 700]
+    cache, table, q, keys, values = build(lens, [1] * 3, heads, kv_heads, 128, 32, "bf16", seed=2)
+    keys[1][1] = keys[1][0]                       # two weights of one half
+    for s in range(3):
+        values[s][lens[s] // 2, :, 3], values[s][0, :, 9] = math.inf, -math.inf
+        put(cache, table, s, 0, keys[s], values[s], 0)
+    got = cache.attention(0, q)
+    cache.poll()
+    assert (got[:, :, 3] == math.inf).all() and (got[:, :, 9] == -math.inf).all()
+    rest = [d for d in range(128) if d not in (3, 9)]
+    for s in range(3):
+        v = values[s].clone()
+        v[:, :, [3, 9]] = 0
+        ref, _, absv, absqk = attend(q[s:s + 1], keys[s], v, np.array([lens[s] - 1]))
+        assert ((got[s:s + 1].double() - ref).abs() <= tolerance(q.dtype, ref, absv, absqk, lens[s], 128 ** -0.5))[:, :, rest].all()
