@@ -153,6 +153,12 @@ template <int N> __device__ __forceinline__ float add_values(Sums& a, const floa
   return m;
 }
 
+// Most tokens that groups of PER threads find: the top-th largest of the groups' maxima is the bound.
+constexpr int most_top(int per) { return LP_THREADS / per; }
+constexpr int LP_FEW_TOP = 32, LP_FEW = 8, LP_MANY = 4;   // threads of a group for up to LP_FEW_TOP tokens, and for more
+static_assert(most_top(LP_FEW) >= LP_FEW_TOP && most_top(LP_MANY) >= LOGPROB_MAX_TOP && LOGPROB_MAX_TOP <= LP_GROUPS && 8 * LOGPROB_MAX_TOP <= LP_LIST,
+              "groups enough for the bound, room for the lists of a row's eight CTAs");
+
 // PER: threads of a group.
 template <typename T, int PER>
 __global__ void __launch_bounds__(LP_THREADS, sizeof(T) == 2 ? 3 : 0) logprob_kernel(LogprobArgs a) {
@@ -244,6 +250,7 @@ __global__ void __launch_bounds__(LP_THREADS, sizeof(T) == 2 ? 3 : 0) logprob_ke
   if (a.top) {
     // the bound: the group maximum that is the top-th largest (equal ones write the same); a group's threads share the others
     constexpr int GROUPS = LP_THREADS / PER;
+    static_assert(GROUPS <= LP_GROUPS && GROUPS % (4 * PER) == 0 && 32 % PER == 0, "a thread's share of the maxima is read 16 bytes at a time");
     const float g = s_group[t / PER];
     int above = 0, not_below = 0;
 #pragma unroll
@@ -385,8 +392,8 @@ cudaError_t launch_logprobs(int dtype, const LogprobArgs& a, cudaStream_t st) {
   cfg.numAttrs = 2;
   // up to 32 tokens are found with 64 groups (1296 x 32000, top 20: 39.8 us against 46.4 with 128; top 64: 94 against 56)
   auto go = [&](auto kernel) { return cudaLaunchKernelEx(&cfg, kernel, a); };
-  const cudaError_t e = dtype == RD_DTYPE_FP32 ? (a.top <= 32 ? go(logprob_kernel<float, 8>) : go(logprob_kernel<float, 4>))
-                                               : (a.top <= 32 ? go(logprob_kernel<__nv_bfloat16, 8>) : go(logprob_kernel<__nv_bfloat16, 4>));
+  const cudaError_t e = dtype == RD_DTYPE_FP32 ? (a.top <= LP_FEW_TOP ? go(logprob_kernel<float, LP_FEW>) : go(logprob_kernel<float, LP_MANY>))
+                                               : (a.top <= LP_FEW_TOP ? go(logprob_kernel<__nv_bfloat16, LP_FEW>) : go(logprob_kernel<__nv_bfloat16, LP_MANY>));
   return e ? e : cudaGetLastError();
 }
 
