@@ -286,3 +286,27 @@ def test_empty_lists_change_nothing():
     assert cache.launch_count() == launches
     for a, b in zip(before, (cache.page_table, cache.lens, cache.refs, cache.free_bits)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("head_dim,dtype", [(64, "fp32"), (128, "bf16")])
+def test_copies_of_many_sequences(head_dim, dtype):
+    """Lists beyond what one entry a thread takes: which shared page is copied to which, and which sharer keeps it, pool bit by bit."""
+    S, page = 700, 16
+    cache, model = make(layers=2, kv_heads=2, head_dim=head_dim, page=page, n_pages=1900, max_seqs=S, max_pages=4, dtype=dtype)
+    rng = np.random.default_rng(head_dim)
+    parents = list(range(20))
+    grow(cache, model, parents, rng.integers(1, 40, len(parents)).tolist(), rng)
+    src, dst = rng.integers(0, 18, 620).tolist(), list(range(20, 640))      # (18 and 19 stay alone)
+    cache.fork(dev(np.array(src)), dev(np.array(dst)))
+    model.fork(src, dst)
+    order = [s for s in rng.permutation(640).tolist() if s % 7]             # some sharers do not write
+    n_new = rng.integers(0, 20, len(order)).tolist()
+    cache.extend(dev(np.array(n_new)), seqs=dev(np.array(order)))
+    assert model.extend(order, n_new)
+    model.check(cache)
+    rest = [s for s in range(640) if s % 7 == 0] + order[:300]
+    n_new = rng.integers(0, 3, len(rest)).tolist()
+    cache.extend(dev(np.array(n_new)), seqs=dev(np.array(rest)))
+    assert model.extend(rest, n_new)
+    model.check(cache)
+    cache.poll()

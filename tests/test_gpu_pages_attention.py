@@ -510,3 +510,17 @@ def test_infinite_values_that_a_single_token_sees(heads, kv_heads):
         v[:, :, [3, 9]] = 0
         ref, _, absv, absqk = attend(q[s:s + 1], keys[s], v, np.array([lens[s] - 1]))
         assert ((got[s:s + 1].double() - ref).abs() <= tolerance(q.dtype, ref, absv, absqk, lens[s], 128 ** -0.5))[:, :, rest].all()
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("n,m", [(1, 128), (20, 256), (40, 400), (127, 255)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (50, 3)])
+def test_many_rows_before_the_first_token(page, n, m, window, sinks):
+    """Rows up to 255 places before a sequence's first token, in tiles that other rows of the item fill with keys."""
+    cache, table, _, keys, values = build([n], [1], 4, 2, 128, page, "bf16")
+    q = torch.randn(m, 4, 128, device="cuda:0").to(torch.bfloat16)
+    lse = torch.zeros(m, 4, device="cuda:0")
+    out = cache.attention(0, q, row_off=dev(np.array([0, m])), max_rows=m, lse=lse, window=window, sinks=sinks)
+    cache.poll()
+    assert (out[:m - n] == 0).all() and (lse[:m - n] == -math.inf).all()
+    compare(out[m - n:], lse[m - n:], q[m - n:], keys, values, [n], [n], window, sinks)
