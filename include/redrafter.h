@@ -419,7 +419,7 @@ RD_API int redrafter_pages_write(rd_pages* h, int32_t layer, const int32_t* seqs
  * boundaries, not overlapping; rows behind the last sequence's are left as they are.  lse: [n_rows][n_heads] fp32, the natural
  * logarithm of the softmax's denominator, or NULL.  scale 0: head_dim^-1/2.  max_rows: the most rows of any sequence, which
  * picks the kernel (the rows of a sequence that brings more are left as they are and reported); 0: n_rows.  A row that would see a page which the table does not name (trimmed too
- * early, say) is reported and not defined.  At most 1024 query heads to a key and value head.  A row without keys (an empty sequence,
+ * early, say) is reported and not defined.  At most 1024 query heads to a key and value head; (n + n_rows) * n_heads < 2^31.  A row without keys (an empty sequence,
  * or all its scores -inf) gives zeros and -inf.  Keys that a row does not see do not reach it, whatever they hold.  Sums and the
  * softmax's statistics are in fp32; bf16: the weights that multiply V are rounded to bf16. */
 RD_API int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, const int32_t* row_off, int32_t n, int32_t n_rows, int32_t max_rows,

@@ -305,6 +305,7 @@ int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, c
   if (window < 0 || sinks < 0) return fail(h, RD_ERR_INVALID_ARG, "window %d, sinks %d", window, sinks);
   if (!std::isfinite(scale) || scale < 0.f) return fail(h, RD_ERR_INVALID_ARG, "scale %g", (double)scale);
   if (max_rows < 0) return fail(h, RD_ERR_INVALID_ARG, "max_rows %d", max_rows);
+  if (((long long)n + n_rows) * n_heads >= (1ll << 31)) return fail(h, RD_ERR_SHAPE, "%d sequences and %d rows of %d heads", n, n_rows, n_heads);   // (the fp32 kernel's grid)
   if (n == 0 || n_rows == 0) return RD_OK;
   if (!q || !out) return fail(h, RD_ERR_INVALID_ARG, "q or out is null");
   const long long row = (long long)n_heads * h->pv.hd;

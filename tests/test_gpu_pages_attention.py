@@ -524,3 +524,15 @@ def test_many_rows_before_the_first_token(page, n, m, window, sinks):
     cache.poll()
     assert (out[:m - n] == 0).all() and (lse[:m - n] == -math.inf).all()
     compare(out[m - n:], lse[m - n:], q[m - n:], keys, values, [n], [n], window, sinks)
+
+
+def test_more_sequences_and_heads_than_a_grid_takes():
+    """Refused on the host, before anything is looked at."""
+    for dtype in ("fp32", "bf16"):
+        cache, table, q, keys, values = build([20], [1], 64, 1, 64, 16, dtype)
+        n = cache.launch_count()
+        for entries in (2 ** 25, 2 ** 31 - 1):
+            rc = cache.L.redrafter_pages_attention(cache.h, 0, None, cache.lens.data_ptr(), entries, 1, 2, 64, q.data_ptr(), 64 * 64, q.data_ptr(), 64 * 64, None,
+                                                   0.0, 0, 0, None)
+            assert rc == 2
+        assert cache.launch_count() == n
