@@ -344,7 +344,7 @@ RD_API int redrafter_route_counts(const rd_handle* h, int64_t* out, int32_t n);
  * goes for graphs that captured them, too).  All but poll may be captured.  A list of sequences `seqs` is a device array of
  * n rows of the table, or NULL: 0 .. n-1.  What a kernel finds out of range -- a sequence outside the table, a length, a
  * page, a row, a sequence named twice by a call that changes it -- it leaves out, and the next redrafter_pages_poll
- * reports it.  Errors of every call: INVALID_ARG, SHAPE, CUDA, STATE (another device than the handle's is current). */
+ * reports it (trim and free, which a second time would change nothing, take such a sequence once).  Errors of every call: INVALID_ARG, SHAPE, CUDA, STATE (another device than the handle's is current). */
 typedef struct {
   int32_t struct_bytes;                       /* sizeof(rd_page_cache) */
   int32_t n_layers, n_kv_heads, head_dim;     /* head_dim 64 or 128 */
@@ -421,7 +421,8 @@ RD_API int redrafter_pages_write(rd_pages* h, int32_t layer, const int32_t* seqs
  * picks the kernel (the rows of a sequence that brings more are left as they are and reported); 0: n_rows.  A row that would see a page which the table does not name (trimmed too
  * early, say) is reported and not defined.  At most 1024 query heads to a key and value head; (n + n_rows) * n_heads < 2^31.  A row without keys (an empty sequence,
  * or all its scores -inf) gives zeros and -inf.  Keys that a row does not see do not reach it, whatever they hold.  Sums and the
- * softmax's statistics are in fp32; bf16: the weights that multiply V are rounded to bf16. */
+ * softmax's statistics are in fp32; bf16: the weights that multiply V are held in two bf16 parts for single tokens (max_rows 1; off by
+ * 2^-16 of a weight at most), rounded to bf16 (2^-8) for more rows. */
 RD_API int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, const int32_t* row_off, int32_t n, int32_t n_rows, int32_t max_rows,
                                      int32_t n_heads, const void* q, int64_t q_stride, void* out, int64_t out_stride, float* lse, float scale,
                                      int32_t window, int32_t sinks, void* stream);

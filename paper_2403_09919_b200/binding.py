@@ -573,7 +573,9 @@ class PagedCache:
         return t.data_ptr(), row if shape[0] > 1 else max(row, shape[1] * shape[2])
 
     def write(self, layer, k, v, row_off=None, seqs=None, max_rows=None):
-        """K and V [rows, kv heads, head dim] of the last tokens of sequences into their pages."""
+        """K and V [rows, kv heads, head dim] of the last tokens of sequences into their pages.
+
+        max_rows: taken as attention takes it, so that one set of arguments serves both; writing does not depend on it."""
         rows = k.shape[0]
         n = rows if row_off is None else row_off.numel() - 1
         shape = (rows, self.n_kv_heads, self.head_dim)

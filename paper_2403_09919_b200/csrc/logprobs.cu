@@ -13,10 +13,11 @@
 // reaches the bound, and the list is ranked by counting.  Where fewer than k groups hold anything above -inf, what is above it
 // and the first 1024 elements are listed.  Rows with NaN or +inf, and lists that overflow, take one maximum after another.
 //
-// Bound by instructions where there are many rows: a thread takes batches of four pieces, with one maximum, one comparison and at most
-// one change of reference a batch, and packed fp32 (a comparison and two selections for each element's place alone had made the scan
-// several times as long).  1296 rows of 32000 in fp32, top 20: 38.3 us, 0.66 of a copy's rate; 6 rows 6.0 us, the chain of a first
-// load, the bound, the list and its ranks.
+// A thread takes batches of four pieces, with one maximum, one comparison and at most one change of reference a batch, and packed fp32 (a
+// comparison and two selections for each element's place alone had made the scan several times as long).  1296 rows of 32000 in fp32,
+// top 20: 38.3 us, 0.66 of a copy's rate.  No unit is at its limit there (issue slots 47 %, exponentials' pipe 28 %, DRAM 49 % of ncu's
+// peak): a row's tail -- bound, list, ranks, a barrier each -- loads nothing, and the SM's two other CTAs hide only a part of it.  6 rows
+// 6.0 us, the chain of a first load and that tail.
 #include <cooperative_groups.h>
 
 #include "logprobs.cuh"

@@ -7,9 +7,10 @@
 // by a cluster of up to 8 CTAs where there are few tiles, joined over distributed shared memory in their order.  Keys that a row
 // does not see take part in nothing: scores are selected, and chunks that only some rows see add V under the rows' masks.
 //
-// Bounds: multiply-adds of the CUDA cores where there are many tiles (8 sequences of 2000 tokens, 256 rows, 4 heads of 64: 208 us,
-// 20 TFLOP/s), else the chain of a tile's chunks, some 1.1 us each (256 rows of 8192 tokens 143 us, of 1000 tokens 24.5; a warp a row
-// and head took 2134 and 260).
+// Bounds: instruction issue where there are many tiles (8 sequences of 2000 tokens, 256 rows, 4 heads of 64: 208 us, 20 of the CUDA
+// cores' 74 TFLOP/s; issue slots 68 % while a CTA is there, 97 on the busiest SM, multiply-adds 39; 512 CTAs of which 444 fit at a
+// time), else the chain of a tile's chunks, some 1.1 us each (256 rows of 8192 tokens 143 us, of 1000 tokens 24.5; a warp a row and head
+// took 2134 and 260).
 #include <cooperative_groups.h>
 
 #include "pages_attention.cuh"
@@ -199,7 +200,7 @@ cudaError_t pages_attention_fp32_prepare(int hd) {
 
 cudaError_t launch_pages_attention_fp32(const PageView& pv, const PageRows& rows, const PageAttention& a, cudaStream_t st) {
   const long long tiles = (rows.n_rows + (long long)(FR_ROWS - 1) * rows.n) / FR_ROWS * a.heads;   // at most
-  // four CTAs an SM hide a chunk's loads (8 sequences of 2000 tokens, 256 rows: 208 us, with at most two 269; a window of 200 keys,
+  // up to four CTAs an SM (three fit at a time) hide a chunk's loads (8 sequences of 2000 tokens, 256 rows: 208 us, with at most two 269; a window of 200 keys,
   // which more of them would cut too short: 41.6, with eight 48.9)
   int S = 1;
   while (S < FR_MAX_SHARE && tiles * S * 2 <= 4 * 148) S *= 2;

@@ -18,8 +18,8 @@
 //   - An item that crosses CTAs leaves its parts (unscaled output, maximum, sum, fp32) in the workspace; the last CTA to
 //     arrive joins them in the order of the CTAs, so that the result does not depend on who is last.
 // Measured with the write of the tokens' K and V before it (a launch of its own, 4 us of these): 16 sequences, 296 MB of K and V,
-// 61.6 us (4.8 TB/s); 1.29 GB 206 us (6.3 TB/s, 0.96 of a copy); a window of 254 MB 53 us; one sequence of 900 tokens (14.8 MB)
-// 10.2 us, a chain of latencies: the write's, three looks into the tables, a page's copy, the products, the join.
+// 62.2 us (4.8 TB/s); 1.29 GB 207 us (6.2 TB/s, 0.95 of a copy); a window of 254 MB 53.5 us; one sequence of 900 tokens (14.8 MB)
+// 10.3 us, a chain of latencies: the write's, three looks into the tables, a page's copy, the products, the join.
 // Keys outside the row's sight are masked by selection and their V is replaced by zeros bit by bit: they may hold anything.
 #include <cuda.h>
 
