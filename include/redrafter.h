@@ -468,8 +468,8 @@ RD_API const char* redrafter_token_logprobs_error(void);   /* why the last one f
  * freed, the state set to match (redrafter_set_state): sequences that share a prompt run it once.  Contexts are bounded by
  * max_seq_pages * page_size instead of max_ctx; too few free pages are reported by redrafter_pages_poll, and what the call that
  * met them computes is not defined.  Speculative calls (draft, pack, verify, accept, step) return STATE meanwhile.
- * pages == NULL: back to the handle's own cache; contexts of prompts and steps that ran on pages are not in it, so that calls return
- * STATE until redrafter_prefill or redrafter_set_state with contexts.  Enqueues nothing.  The pages have to outlive their use.
+ * pages == NULL: back to the handle's own cache; contexts that prompts, steps or redrafter_set_state left while pages were in use are not
+ * in it, so that calls return STATE until redrafter_prefill or redrafter_set_state with contexts.  Enqueues nothing.  The pages have to outlive their use.
  * Errors: UNSUPPORTED (fp32, RD_FLAG_FORCE_SIMT), SHAPE (pages of another model), INVALID_ARG, STATE (another device). */
 RD_API int redrafter_use_pages(rd_handle* h, rd_pages* pages, const int32_t* seqs, int32_t window, int32_t sinks);
 

@@ -1351,7 +1351,7 @@ int redrafter_set_state(rd_handle* h, void* stream, const int32_t* ctx, const in
   if (ctx) {
     CKRT(h, cudaMemcpyAsync(h->ws.ctx, ctx, B * sizeof(int32_t), cudaMemcpyDeviceToDevice, st));
     fb_invalidate(h);   // copies of the old context lengths say nothing about the new ones
-    h->ctx_in_pages = false;
+    h->ctx_in_pages = h->pages != nullptr;
   }
   if (root) CKRT(h, cudaMemcpyAsync(h->ws.root, root, B * sizeof(int32_t), cudaMemcpyDeviceToDevice, st));
   if (hvec) CKRT(h, cudaMemcpyAsync(h->ws.h, hvec, B * h->dm.d * sizeof(float), cudaMemcpyDeviceToDevice, st));

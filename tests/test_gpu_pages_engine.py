@@ -470,3 +470,23 @@ def test_a_closed_cache_is_refused():
     r.eng.prefill([np.arange(10)])
     r.eng.step()
     r.eng.poll()
+
+
+def test_contexts_set_while_pages_are_in_use_are_those_of_the_pages():
+    """A branch's state belongs to the pages, though nothing has run on them since."""
+    r = Rig(cfg=CFG)
+    cache = pages_for(CFG, 16)
+    r.eng.use_pages(cache)
+    r.eng.prefill([np.arange(40)])
+    cache.fork(dev(np.array([0])), dev(np.array([1])))
+    r.eng.set_state(dev(np.array([40, 40])), dev(np.array([1, 2])), None, batch=2, ctx_bound=40)
+    r.eng.use_pages(None)
+    for call in (r.eng.step, r.eng.ar_step):
+        with pytest.raises(binding.RdError) as e:
+            call()
+        assert e.value.code == 4
+    r.eng.use_pages(cache)
+    r.eng.ar_step()
+    r.eng.poll()
+    cache.poll()
+    assert cache.lens.tolist()[:2] == [41, 41]
