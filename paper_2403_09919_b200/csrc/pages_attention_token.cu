@@ -19,7 +19,7 @@
 //     arrive joins them in the order of the CTAs, so that the result does not depend on who is last.
 // Measured with the write of the tokens' K and V before it (a launch of its own, 4 us of these): 16 sequences, 296 MB of K and V,
 // 62.2 us (4.8 TB/s); 1.29 GB 207 us (6.2 TB/s, 0.95 of a copy); a window of 254 MB 53.5 us; one sequence of 900 tokens (14.8 MB)
-// 10.3 us, a chain of latencies: the write's, three looks into the tables, a page's copy, the products, the join.
+// 10.1 us, a chain of latencies: the write's, three looks into the tables, a page's copy, the products, the join.
 // Keys outside the row's sight are masked by selection and their V is replaced by zeros bit by bit: they may hold anything.
 #include <cuda.h>
 
@@ -38,10 +38,11 @@ constexpr int TK_WARPS = 4;          // consumer warps, 16 keys each
 constexpr int TK_THREADS = TK_WARPS * 32 + 32;
 constexpr int TK_STAGES = 6;
 // Units that a CTA takes at least where an item is cut, and chunks of an item that is not: the more rows a part has, the longer the
-// join of many (900 tokens of 32 heads: 8.3 us with 3, 8.7 with 4, 10.0 with 6; 16384 tokens of 16 query heads on one: 27.1 with 6,
-// 20.7 with 10; fp32, whose chunks take longer, 1000 tokens of 4 heads: 9.7 with 1, 12.5 with 3).
+// join of many (900 tokens of 32 heads: 8.5 us with 3, 9.2 with 4, 10.0 with 6; 16 query heads on one, 16384 tokens: 28.3 with 6, 22.6
+// with 10, 40000: 55.8 and 39.2, but 16 sequences of 2000: 14.8 and 18.2; fp32, whose chunks take longer, 1000 tokens of 4 heads: 7.8 with
+// 1, 10.7 with 3).
 constexpr int TK_MIN_UNITS = 3, TK_MIN_UNITS_WIDE = 10, TK_WHOLE = 10;
-constexpr int TK_JOIN = 16;          // parts that a thread of the join has under way
+constexpr int TK_JOIN = 8, TK_REST = 2;   // parts that a thread of the join has under way; parts left that it takes one by one
 
 struct TokenParams {
   PageView pv;
@@ -270,47 +271,59 @@ __device__ __forceinline__ void join_warps(const TokenParams& p, const float* s_
   }
 }
 
-// The parts of an item joined in the order of its CTAs, by the consumers of the last one to arrive: TK_JOIN parts' loads under way at
-// a time, the last batch filled up with its last part (a rest one by one took 0.4 us for each; 18 parts: 11.5 us, with it 13.2).
+// The parts of an item joined in the order of its CTAs, by the consumers of the last one to arrive: TK_JOIN parts' loads under way at a
+// time, the last batch filled up with the last part, and up to TK_REST that are left one by one.  What fills a batch up is selected away and
+// not branched over: the compiler moves the loads behind the branches, one after another (16384 tokens of 16 query heads on one: 32.4 us,
+// this 22.7; 8000 of 32 on 8, 18 parts: 13.9, 11.7).  Sixteen at a time: 40000 tokens of 16 on one 31.8 us for 39.9, but one user's 900
+// tokens (three parts) 10.45 for 10.1; four: 56 and 9.9.
 template <typename T, int HD>
 __device__ __forceinline__ void join_parts(const TokenParams& p, int first_cta, int last_cta, int row_out, long long head0, int q_rows) {
   constexpr int PITCH = HD + 4;
   const size_t step = (size_t)2 * 16 * PITCH;
+  const int others = last_cta - first_cta;
+  auto batches = [&](auto take) {   // take(first, constant of the batch's size)
+    int k0 = 0;
+    for (; others - k0 > TK_REST; k0 += TK_JOIN) take(k0, std::integral_constant<int, TK_JOIN>{});
+#pragma unroll 1
+    for (; k0 < others; ++k0) take(k0, std::integral_constant<int, 1>{});
+  };
   for (int e = threadIdx.x; e < q_rows * (HD / 4); e += TK_WARPS * 32) {
     const int row = e / (HD / 4), d = (e - row * (HD / 4)) * 4;
     const float* at0 = p.parts + ((size_t)first_cta * 2 + 1) * 16 * PITCH + row * PITCH;   // the first CTA's slot 1, the others' slot 0
     const float* at = p.parts + (size_t)(first_cta + 1) * step + row * PITCH;
-    const int others = last_cta - first_cta;
     float M = __ldcg(at0 + HD);
-    for (int k0 = 0; k0 < others; k0 += TK_JOIN) {
-      float x[TK_JOIN];
+    batches([&](int k0, auto size) {
+      constexpr int N = decltype(size)::value;
+      float x[N];
 #pragma unroll
-      for (int k = 0; k < TK_JOIN; ++k) x[k] = __ldcg(at + min(k0 + k, others - 1) * step + HD);
+      for (int k = 0; k < N; ++k) x[k] = __ldcg(at + min(k0 + k, others - 1) * step + HD);
 #pragma unroll
-      for (int k = 0; k < TK_JOIN; ++k) M = fmaxf(M, x[k]);
-    }
+      for (int k = 0; k < N; ++k) M = fmaxf(M, x[k]);
+    });
     const float ref = M == -INFINITY ? 0.f : M;
     float f = fast_exp2(__ldcg(at0 + HD) - ref);
     float L = f * __ldcg(at0 + HD + 1);
     float4 v = __ldcg(reinterpret_cast<const float4*>(at0 + d));
     v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-    for (int k0 = 0; k0 < others; k0 += TK_JOIN) {
-      float2 st[TK_JOIN];
-      float4 x[TK_JOIN];
+    batches([&](int k0, auto size) {
+      constexpr int N = decltype(size)::value;
+      float2 st[N];
+      float4 x[N];
 #pragma unroll
-      for (int k = 0; k < TK_JOIN; ++k) {
+      for (int k = 0; k < N; ++k) {
         const float* part = at + min(k0 + k, others - 1) * step;
         st[k] = __ldcg(reinterpret_cast<const float2*>(part + HD));
         x[k] = __ldcg(reinterpret_cast<const float4*>(part + d));
       }
 #pragma unroll
-      for (int k = 0; k < TK_JOIN; ++k) {
-        if (k0 + k >= others) break;
-        f = fast_exp2(st[k].x - ref);
-        L = fmaf(f, st[k].y, L);
-        v.x = fmaf(f, x[k].x, v.x); v.y = fmaf(f, x[k].y, v.y); v.z = fmaf(f, x[k].z, v.z); v.w = fmaf(f, x[k].w, v.w);
+      for (int k = 0; k < N; ++k) {
+        const bool there = k0 + k < others;
+        f = there ? fast_exp2(st[k].x - ref) : 0.f;
+        L = fmaf(f, there ? st[k].y : 0.f, L);
+        v.x = fmaf(f, there ? x[k].x : 0.f, v.x); v.y = fmaf(f, there ? x[k].y : 0.f, v.y);
+        v.z = fmaf(f, there ? x[k].z : 0.f, v.z); v.w = fmaf(f, there ? x[k].w : 0.f, v.w);
       }
-    }
+    });
     const float inv = L == 0.f ? 0.f : 1.f / L;
     T* out = reinterpret_cast<T*>(p.a.out) + (long long)row_out * p.a.out_stride + (head0 + row) * HD + d;
     out[0] = from_f<T>(v.x * inv); out[1] = from_f<T>(v.y * inv); out[2] = from_f<T>(v.z * inv); out[3] = from_f<T>(v.w * inv);
