@@ -344,7 +344,8 @@ RD_API int redrafter_route_counts(const rd_handle* h, int64_t* out, int32_t n);
  * goes for graphs that captured them, too).  All but poll may be captured.  A list of sequences `seqs` is a device array of
  * n rows of the table, or NULL: 0 .. n-1.  What a kernel finds out of range -- a sequence outside the table, a length, a
  * page, a row, a sequence named twice by a call that changes it -- it leaves out, and the next redrafter_pages_poll
- * reports it (trim and free, which a second time would change nothing, take such a sequence once).  Errors of every call: INVALID_ARG, SHAPE, CUDA, STATE (another device than the handle's is current). */
+ * reports it (trim and free, which a second time would change nothing, take such a sequence once).  Errors of every call:
+ * INVALID_ARG, SHAPE, CUDA, STATE (another device than the handle's is current). */
 typedef struct {
   int32_t struct_bytes;                       /* sizeof(rd_page_cache) */
   int32_t n_layers, n_kv_heads, head_dim;     /* head_dim 64 or 128 */
@@ -418,9 +419,9 @@ RD_API int redrafter_pages_write(rd_pages* h, int32_t layer, const int32_t* seqs
  * q, out: [n_rows][n_heads][head_dim] of the cache's dtype, rows q_stride and out_stride elements apart and on 16-byte
  * boundaries, not overlapping; rows behind the last sequence's are left as they are.  lse: [n_rows][n_heads] fp32, the natural
  * logarithm of the softmax's denominator, or NULL.  scale 0: head_dim^-1/2.  max_rows: the most rows of any sequence, which
- * picks the kernel (the rows of a sequence that brings more are left as they are and reported); 0: n_rows.  A row that would see a page which the table does not name (trimmed too
- * early, say) is reported and not defined.  At most 1024 query heads to a key and value head; (n + n_rows) * n_heads < 2^31.  A row without keys (an empty sequence,
- * or all its scores -inf) gives zeros and -inf.  Keys that a row does not see do not reach it, whatever they hold.  Sums and the
+ * picks the kernel (the rows of a sequence that brings more are left as they are and reported); 0: n_rows.  A row that would see a
+ * page which the table does not name (trimmed too early, say) is reported and not defined.  At most 1024 query heads to a key and value
+ * head; (n + n_rows) * n_heads < 2^31.  A row without keys (an empty sequence, or all its scores -inf) gives zeros and -inf.  Keys that a row does not see do not reach it, whatever they hold.  Sums and the
  * softmax's statistics are in fp32; bf16: the weights that multiply V are held in two bf16 parts for single tokens (max_rows 1; off by
  * 2^-16 of a weight at most), rounded to bf16 (2^-8) for more rows. */
 RD_API int redrafter_pages_attention(rd_pages* h, int32_t layer, const int32_t* seqs, const int32_t* row_off, int32_t n, int32_t n_rows, int32_t max_rows,
@@ -469,7 +470,8 @@ RD_API const char* redrafter_token_logprobs_error(void);   /* why the last one f
  * max_seq_pages * page_size instead of max_ctx; too few free pages are reported by redrafter_pages_poll, and what the call that
  * met them computes is not defined.  Speculative calls (draft, pack, verify, accept, step) return STATE meanwhile.
  * pages == NULL: back to the handle's own cache; contexts that prompts, steps or redrafter_set_state left while pages were in use are not
- * in it, so that calls return STATE until redrafter_prefill or redrafter_set_state with contexts.  Enqueues nothing.  The pages have to outlive their use.
+ * in it, so that calls return STATE until redrafter_prefill or redrafter_set_state with contexts.  Enqueues nothing.  The pages have to
+ * outlive their use.
  * Errors: UNSUPPORTED (fp32, RD_FLAG_FORCE_SIMT), SHAPE (pages of another model), INVALID_ARG, STATE (another device). */
 RD_API int redrafter_use_pages(rd_handle* h, rd_pages* pages, const int32_t* seqs, int32_t window, int32_t sinks);
 
@@ -479,8 +481,8 @@ RD_API int redrafter_use_pages(rd_handle* h, rd_pages* pages, const int32_t* seq
  * redrafter_step the accepted tokens and the bonus token, columns 0 .. n_accept[b]; after redrafter_ar_step and
  * redrafter_prefill (the root) column 0.  The other columns are NaN and -1.  What was emitted is recorded on the device by the call's
  * own launches: after a replay of a captured step it is the replay's.  A verification, an acceptance and redrafter_set_state end it.
- * Errors: STATE when the last of these calls emitted nothing; on a handle of which an emitting call has been captured, whose
- * replays the host does not see, all columns are NaN and -1 then. */
+ * Errors: STATE when the last of these calls emitted nothing; all columns are NaN and -1 then where one of them has been captured,
+ * whose replays the host does not see. */
 RD_API int redrafter_last_logprobs(rd_handle* h, void* stream, int32_t top, float temperature, float* logprob, float* entropy, int32_t* top_ids,
                                    float* top_logprobs);
 
